@@ -302,6 +302,106 @@ int moss_gemm_fp8_mx(int64_t M, int64_t N, int64_t K,
 int moss_gemm_bf16_baseline(int64_t M, int64_t N, int64_t K, const void *a_bf16, const void *b_bf16,
                             void *out_bf16, int64_t ld_out, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * The recipe with one FP32 scale per block of 128 elements, the per-group scheme that the paper compares MOSS
+ * with (Sec. 1, Sec. 3.1): its quantizers and its products.  For every group or block of elements
+ *      s = fl32(amax / 448)  (1 if all are zero),
+ *      code = E4M3 of fl32(x * fl32(1/s)), rounded to nearest even, saturated to +-448, sign kept
+ * (fl32(1/s) is capped at FLT_MAX).  No scale depends on the whole tensor: every input is read once, in one launch
+ * without a workspace.
+ *
+ * moss_quant_block128: activations and gradients, BF16 [rows x cols], row stride `ld`.
+ *   MOSS_Q_ROW: groups of 128 along the columns: q_row [rows x cols], s_row [rows x ceil(cols/128)].
+ *   MOSS_Q_COL: groups of 128 along the rows, stored transposed: q_col [cols x rows], s_col [cols x ceil(rows/128)].
+ *   The last group of a row (column) holds what is left.
+ * moss_quant_block128_weight: weights, FP32 or BF16 [rows x cols] dense, in blocks of 128 x 128:
+ *   wq [rows x cols], s [ceil(rows/128) x ceil(cols/128)], and optionally (wq_t not NULL) the transposed codes
+ *   wq_t [cols x rows] with s_t [ceil(cols/128) x ceil(rows/128)], the operand of dX = dY W.
+ * Requirements: cols % 32 == 0; rows % 32 == 0 if anything transposed is asked for; ld >= cols, ld % 8 == 0; finite
+ * inputs; no other flags (else MOSS_ERR_UNSUPPORTED).  Scale arrays are 4-byte aligned.
+ * ------------------------------------------------------------------------- */
+int moss_quant_block128(const void *x_bf16, int64_t rows, int64_t cols, int64_t ld, unsigned flags, uint8_t *q_row, float *s_row,
+                        uint8_t *q_col, float *s_col, void *stream);
+int moss_quant_block128_weight(const void *w, int w_dtype, int64_t rows, int64_t cols, uint8_t *wq, float *s, uint8_t *wq_t,
+                               float *s_t, void *stream);
+
+/*   out[m,n] (+)= sum_j a_s[m,j] b_s[n / b_block, j] * sum_{k in block j} dec(a_q[m,k]) dec(b_q[n,k])
+ *   a_q [M x K], b_q [N x K]   E4M3 codes, both K-contiguous, dense; block j is k in [128 j, 128 j + 128), the last
+ *                               one what is left of K.
+ *   a_s [M x ceil(K/128)]; b_s [ceil(N/128) x ceil(K/128)] (b_block 128, a weight) or [N x ceil(K/128)] (b_block 1).
+ *   out  [M x N], row stride ld_out elements, BF16 or FP32; accumulate != 0 adds into an FP32 `out`.
+ * The three products of a linear layer:
+ *   Y = X W^T: (Xq_row, s_row), (Wq, s), 128;  dX = dY W: (dYq_row, s_row), (Wq_t, s_t), 128;
+ *   dW = dY^T X: (dYq_col, s_col), (Xq_col, s_col), 1.
+ * The product of two scales is capped at FLT_MAX.  A block's products are summed by the matrix unit, the blocks in FP32 in order of K (K split in up to four parts, each in order,
+ * where the problem is small: the choice goes by sizes alone).
+ * Requirements: K % 32 == 0, K <= 2^22; ld_out >= N; 16-byte aligned codes and out. */
+int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, const float *a_s, const uint8_t *b_q, const float *b_s,
+                           int64_t b_block, void *out, int out_dtype, int64_t ld_out, int accumulate, void *stream);
+
+/* ---------------------------------------------------------------------------
+ * A layer of experts.  Routing sends every token to k of `groups` experts; the rows of an expert lie side by side, and how
+ * many there are stands in device memory only:
+ *   offsets  [groups + 1] int32: group g has the rows offsets[g] .. offsets[g+1] - 1; none if the two are equal.  They
+ *            must not decrease.  (Whatever they are, nothing is read or written beyond `rows`; which outputs a wrong array
+ *            leaves unwritten is unspecified.)
+ * moss_gemm_fp8_mx_grouped: forward and dX, every group with a weight of its own,
+ *      out[r,n] (+)= a_s b_s[g] * sum_k dec(a_q[r,k]) 2^(a_e[r,k/32]-127) dec(b_q[g][n,k])      for r in group g.
+ *   a_q [rows x K], a_e [rows x K/32] (NULL: unit), a_s one scale: the two-level quantizer's, over all rows.
+ *   b_q  byte n, k of group g at b_q + g b_stride + n ld_b + k; b_s[g b_s_stride] its scale.  Weights of their own:
+ *        ld_b = K, b_stride = N K; the transposed codes [K x groups N] of one stacked weight: ld_b = groups K, b_stride = K;
+ *        b_s_stride 0: one scale for all; moss_wscale_state arrays: b_s = &state[0].s_cur, b_s_stride = sizeof / 4.
+ *   out  [rows x N], row stride ld_out, BF16 or FP32.  Rows of no group stay as they were.
+ *   Requirements: K % 32 == 0, K <= 2^22, K <= ld_b <= 2^24, ld_b and b_stride multiples of 16 and not negative.
+ * moss_gemm_fp8_mx_grouped_dw: the weight gradients, groups along the inner dimension,
+ *      out[g][m,n] (+)= a_s b_s * sum_{r in group g} dec(a_q[m,r]) 2^(a_e[m,r/32]-127) dec(b_q[n,r]) 2^(b_e[n,r/32]-127).
+ *   a_q [M x rows], a_e [M x rows/32], b_q [N x rows], b_e [N x rows/32]: column groupings of the two-level quantizer.
+ *   out  [groups x M x N] dense; a group without rows gets zeros (or, accumulating, stays as it is).
+ *   Requirements: rows % 32 == 0, rows <= 2^24, offsets that are multiples of 32.
+ * Both: groups <= 1024, BF16 or FP32 outputs, accumulate only with FP32; otherwise as moss_gemm_fp8_mx.
+ * ------------------------------------------------------------------------- */
+int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
+                             const uint8_t *a_e, const float *a_s, const uint8_t *b_q, int64_t ld_b, int64_t b_stride,
+                             const float *b_s, int64_t b_s_stride, void *out, int out_dtype, int64_t ld_out, int accumulate,
+                             void *stream);
+int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
+                                const uint8_t *a_e, const float *a_s, const uint8_t *b_q, const uint8_t *b_e, const float *b_s,
+                                void *out, int out_dtype, int accumulate, void *stream);
+
+/* The rows' way to the experts and back.
+ *
+ * moss_expert_rows: how many rows the assignments of `tokens` tokens to k experts each take at most, every expert's filled
+ * up to `multiple` (0 for bad arguments).  The column groupings need multiples of 32; forward alone needs 1.
+ *
+ * moss_expert_plan: experts [tokens x k] int32, any order, the same one twice allowed; a number outside [0, n_experts) drops the
+ * assignment.  The assignments (t, j), numbered t k + j, of expert 0 come first, in order, then those of expert 1, ..., each
+ * expert's rows filled up to `multiple`; the last expert also has the rows that are left over.
+ *   row_of  [tokens x k]: the row of every assignment (-1: dropped);
+ *   source  [rows]: the assignment of every row (-1: a row without one);
+ *   offsets [n_experts + 1]: first rows; offsets[n_experts] = rows.
+ *   Requirements: rows >= moss_expert_rows(...), a multiple of `multiple`; n_experts <= 1024, multiple <= 4096.
+ *
+ * moss_expert_dispatch_bf16: y[row_of[t,j]] = x[t], zeros in rows without an assignment; *y_absmax_bits: max|y| as the other
+ * producers leave it.  Its gradient is moss_expert_combine_bf16 without weights.
+ * moss_expert_combine_bf16: out[t] = sum_j weights[t,j] * y[row_of[t,j]] (weights NULL: 1), FP32 in the order of j, one rounding;
+ * dropped assignments add nothing, rows without one are not read.
+ * moss_expert_combine_bf16_backward: d_y[row_of[t,j]] = weights[t,j] * d_out[t] (rounded once), zeros elsewhere, with its maximum
+ * word; d_weights[t,j] = sum_c d_out[t,c] y[row_of[t,j],c] in FP32 (0 if dropped).  d_y has the row stride of y.
+ *
+ * x, out, d_out: BF16 [tokens x cols]; y, d_y: BF16 [rows x cols]; weights, d_weights: FP32 [tokens x k] dense.
+ * Requirements: cols % 8 == 0, row strides >= cols and multiples of 8, finite inputs.  Entries of row_of and source outside their
+ * ranges count as -1; a row_of with one row twice, or a source that does not belong to it, leaves unspecified values.      */
+int64_t moss_expert_rows(int64_t tokens, int64_t k, int64_t n_experts, int64_t multiple);
+int moss_expert_plan(const int32_t *experts, int64_t tokens, int64_t k, int64_t n_experts, int64_t multiple, int64_t rows,
+                     int32_t *row_of, int32_t *source, int32_t *offsets, void *stream);
+int moss_expert_dispatch_bf16(const void *x, const int32_t *row_of, const int32_t *source, int64_t tokens, int64_t k, int64_t rows,
+                              int64_t cols, int64_t ld_x, int64_t ld_y, void *y, uint32_t *y_absmax_bits, void *stream);
+int moss_expert_combine_bf16(const void *y, const int32_t *row_of, const float *weights, int64_t tokens, int64_t k, int64_t rows,
+                             int64_t cols, int64_t ld_y, int64_t ld_out, void *out, void *stream);
+int moss_expert_combine_bf16_backward(const void *d_out, const void *y, const int32_t *row_of, const int32_t *source,
+                                      const float *weights, int64_t tokens, int64_t k, int64_t rows, int64_t cols, int64_t ld_out,
+                                      int64_t ld_y, void *d_y, float *d_weights, uint32_t *d_y_absmax_bits, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

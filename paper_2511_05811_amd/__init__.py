@@ -9,4 +9,6 @@ from .binding import (  # noqa: F401
     AdamWArgs, MossError, WScaleState, device_cu_count, exported_symbols, gemm_bf16_baseline,
     gemm_fp8_mx, lib_path, load, quant_act_2level, quant_act_2level_given_max, quant_act_2level_noalloc, quant_set_poll_limit, read_wscale_state, weight_autoscale_cast,
     weight_autoscale_init, new_wscale_state, swiglu_bf16, swiglu_bf16_backward, add_rmsnorm_bf16, rmsnorm_bf16_backward,
+    quant_block128, quant_block128_weight, gemm_fp8_block128, gemm_fp8_mx_grouped, gemm_fp8_mx_grouped_dw,
+    expert_rows, expert_plan, expert_dispatch_bf16, expert_combine_bf16, expert_combine_bf16_backward,
 )

@@ -81,6 +81,17 @@ def load():
     L.moss_gemm_workspace_bytes.argtypes = [i64, i64, i64]
     L.moss_gemm_fp8_mx.argtypes = [i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, ci, i64, ci, vp, sz, vp]
     L.moss_gemm_bf16_baseline.argtypes = [i64, i64, i64, vp, vp, vp, i64, vp]
+    L.moss_quant_block128.argtypes = [vp, i64, i64, i64, u32, vp, vp, vp, vp, vp]
+    L.moss_quant_block128_weight.argtypes = [vp, ci, i64, i64, vp, vp, vp, vp, vp]
+    L.moss_gemm_fp8_block128.argtypes = [i64, i64, i64, vp, vp, vp, vp, i64, vp, ci, i64, ci, vp]
+    L.moss_gemm_fp8_mx_grouped.argtypes = [i64, i64, i64, i64, vp, vp, vp, vp, vp, i64, i64, vp, i64, vp, ci, i64, ci, vp]
+    L.moss_gemm_fp8_mx_grouped_dw.argtypes = [i64, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, ci, ci, vp]
+    L.moss_expert_rows.restype = i64
+    L.moss_expert_rows.argtypes = [i64, i64, i64, i64]
+    L.moss_expert_plan.argtypes = [vp, i64, i64, i64, i64, i64, vp, vp, vp, vp]
+    L.moss_expert_dispatch_bf16.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, vp, vp]
+    L.moss_expert_combine_bf16.argtypes = [vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, vp]
+    L.moss_expert_combine_bf16_backward.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, i64, vp, vp, vp, vp]
     _lib = L
     return L
 
@@ -426,3 +437,243 @@ def gemm_bf16_baseline(a, b, out=None):
     rc = L.moss_gemm_bf16_baseline(M, N, K, _ptr(a), _ptr(b), _ptr(out), out.stride(0), _stream())
     _check(rc, "moss_gemm_bf16_baseline")
     return out
+
+
+def _same_device(*tensors):
+    """The GPU that all of them are on, which has to be the current one: the calls go to its current stream."""
+    import torch
+    dev = None
+    for t in tensors:
+        if t is not None:
+            assert t.is_cuda and (dev is None or t.device == dev), "tensors on one GPU"
+            dev = t.device
+    assert dev.index == torch.cuda.current_device(), "tensors on the current GPU"
+    return dev
+
+
+def _new(shape, dtype, device, given=None):
+    """The caller's dense tensor of that shape and type, or a new one."""
+    import torch
+    if given is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    assert given.dtype == dtype and tuple(given.shape) == tuple(shape) and given.is_contiguous() and given.device == device
+    return given
+
+
+def _rows_out(out, rows, cols, dtype, device):
+    """A [rows x cols] output whose rows may be further apart than its columns are wide: the caller's or a new one."""
+    import torch
+    if out is None:
+        return torch.empty((rows, cols), dtype=dtype, device=device)
+    assert tuple(out.shape) == (rows, cols) and (cols == 1 or out.stride(1) == 1) and out.device == device
+    return out
+
+
+def _ld(t):
+    """Row stride of a [rows x cols] tensor; that of a single row says nothing."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def quant_block128(x, flags=MOSS_Q_ROW, out=None):
+    """Groups of 128 with an FP32 scale each; x: torch.bfloat16 [rows, cols] on the GPU (row stride may exceed cols).
+    Returns dict(q_row, s_row, q_col, s_col) of device tensors (absent outputs are None)."""
+    import torch
+    L = load()
+    assert x.dtype == torch.bfloat16 and x.dim() == 2 and x.stride(1) == 1
+    dev = _same_device(x)
+    rows, cols = x.shape
+    out = out or {}
+    u8, f32 = torch.uint8, torch.float32
+    got = dict(q_row=None, s_row=None, q_col=None, s_col=None)
+    if flags & MOSS_Q_ROW:
+        got["q_row"] = _new((rows, cols), u8, dev, out.get("q_row"))
+        got["s_row"] = _new((rows, (cols + 127) // 128), f32, dev, out.get("s_row"))
+    if flags & MOSS_Q_COL:
+        got["q_col"] = _new((cols, rows), u8, dev, out.get("q_col"))
+        got["s_col"] = _new((cols, (rows + 127) // 128), f32, dev, out.get("s_col"))
+    rc = L.moss_quant_block128(_ptr(x), rows, cols, _ld(x), flags, _ptr(got["q_row"]), _ptr(got["s_row"]), _ptr(got["q_col"]),
+                               _ptr(got["s_col"]), _stream())
+    _check(rc, "moss_quant_block128")
+    return got
+
+
+def quant_block128_weight(w, want_transpose=False, wq=None, s=None, wq_t=None, s_t=None):
+    """(wq, s, wq_t, s_t) of a dense float32 or bfloat16 weight [rows, cols] in blocks of 128 x 128; the transposed two are None
+    unless asked for (or given)."""
+    import torch
+    L = load()
+    assert w.dim() == 2 and w.is_contiguous()
+    dev = _same_device(w)
+    rows, cols = w.shape
+    r, c = (rows + 127) // 128, (cols + 127) // 128
+    wq, s = _new((rows, cols), torch.uint8, dev, wq), _new((r, c), torch.float32, dev, s)
+    if want_transpose or wq_t is not None:
+        wq_t, s_t = _new((cols, rows), torch.uint8, dev, wq_t), _new((c, r), torch.float32, dev, s_t)
+    else:
+        s_t = None
+    rc = L.moss_quant_block128_weight(_ptr(w), _dt(w), rows, cols, _ptr(wq), _ptr(s), _ptr(wq_t), _ptr(s_t), _stream())
+    _check(rc, "moss_quant_block128_weight")
+    return wq, s, wq_t, s_t
+
+
+def gemm_fp8_block128(a_q, a_s, b_q, b_s, out=None, out_dtype=None, accumulate=False):
+    """out[m,n] (+)= sum over blocks of 128 of k of a_s[m,block] b_s[n or n // 128,block] * sum a[m,k] b[n,k]; a_q [M,K], b_q [N,K]
+    uint8, a_s [M,ceil(K/128)], b_s [ceil(N/128),ceil(K/128)] (a weight) or [N,ceil(K/128)], float32, all dense."""
+    import torch
+    L = load()
+    M, K = a_q.shape
+    N = b_q.shape[0]
+    blocks = (K + 127) // 128
+    assert a_q.dtype == b_q.dtype == torch.uint8 and a_s.dtype == b_s.dtype == torch.float32
+    assert b_q.shape[1] == K and tuple(a_s.shape) == (M, blocks) and tuple(b_s.shape) in ((N, blocks), ((N + 127) // 128, blocks))
+    assert all(t.is_contiguous() for t in (a_q, a_s, b_q, b_s))
+    dev = _same_device(a_q, a_s, b_q, b_s, out)
+    out = _rows_out(out, M, N, out_dtype or torch.bfloat16, dev)
+    rc = L.moss_gemm_fp8_block128(M, N, K, _ptr(a_q), _ptr(a_s), _ptr(b_q), _ptr(b_s), 128 if b_s.shape[0] == (N + 127) // 128 else 1,
+                                  _ptr(out), _dt(out), _ld(out), int(bool(accumulate)), _stream())
+    _check(rc, "moss_gemm_fp8_block128")
+    return out
+
+
+def gemm_fp8_mx_grouped(a_q, a_e, a_s, b_q, b_s, offsets, out=None, out_dtype=None, accumulate=False):
+    """Row r of group g (offsets[g] <= r < offsets[g + 1], int32): out[r,n] (+)= a_s*b_s[g]*sum_k a[r,k] 2^(ae-127) b[g,n,k]; a_q [R,K],
+    a_e [R,K/32] or None, a_s a float32 scalar, b_q [G,N,K] (neighbours along K; other strides multiples of 16), b_s [G] float32 of any
+    stride, or one scale for all.  Rows of no group stay as they were."""
+    import torch
+    L = load()
+    R, K = a_q.shape
+    G, N, _ = b_q.shape
+    assert a_q.dtype == b_q.dtype == torch.uint8 and b_q.shape[2] == K and a_q.is_contiguous() and b_q.stride(2) == 1
+    assert a_e is None or (a_e.dtype == torch.uint8 and tuple(a_e.shape) == (R, K // 32) and a_e.is_contiguous())
+    assert a_s.dtype == b_s.dtype == torch.float32 and a_s.numel() == 1 and (b_s.numel() == 1 or tuple(b_s.shape) == (G,))
+    assert offsets.dtype == torch.int32 and tuple(offsets.shape) == (G + 1,) and offsets.is_contiguous()
+    dev = _same_device(a_q, a_e, a_s, b_q, b_s, offsets, out)
+    out = _rows_out(out, R, N, out_dtype or torch.bfloat16, dev)
+    rc = L.moss_gemm_fp8_mx_grouped(R, N, K, G, _ptr(offsets), _ptr(a_q), _ptr(a_e), _ptr(a_s), _ptr(b_q),
+                                    b_q.stride(1) if N > 1 else K, b_q.stride(0) if G > 1 else 0, _ptr(b_s),
+                                    b_s.stride(0) if b_s.numel() > 1 else 0, _ptr(out), _dt(out), _ld(out), int(bool(accumulate)), _stream())
+    _check(rc, "moss_gemm_fp8_mx_grouped")
+    return out
+
+
+def gemm_fp8_mx_grouped_dw(a_q, a_e, a_s, b_q, b_e, b_s, offsets, out=None, out_dtype=None, accumulate=False):
+    """out[g,m,n] (+)= a_s*b_s*sum over r of group g (offsets as above, multiples of 32) of a[m,r] 2^(ae-127) b[n,r] 2^(be-127); a_q [M,R],
+    b_q [N,R] uint8, a_e/b_e uint8 [.,R/32], a_s/b_s float32 scalars.  Without `out` a float32 tensor [G,M,N]."""
+    import torch
+    L = load()
+    M, R = a_q.shape
+    N, G = b_q.shape[0], offsets.numel() - 1
+    assert all(t.dtype == torch.uint8 and t.is_contiguous() for t in (a_q, a_e, b_q, b_e)) and b_q.shape[1] == R
+    assert tuple(a_e.shape) == (M, R // 32) and tuple(b_e.shape) == (N, R // 32)
+    assert a_s.dtype == b_s.dtype == torch.float32 and a_s.numel() == 1 and b_s.numel() == 1
+    assert offsets.dtype == torch.int32 and offsets.dim() == 1 and offsets.is_contiguous()
+    dev = _same_device(a_q, a_e, a_s, b_q, b_e, b_s, offsets, out)
+    if out is None:
+        out = torch.empty((G, M, N), dtype=out_dtype or torch.float32, device=dev)
+    assert tuple(out.shape) == (G, M, N) and out.is_contiguous()
+    rc = L.moss_gemm_fp8_mx_grouped_dw(R, M, N, G, _ptr(offsets), _ptr(a_q), _ptr(a_e), _ptr(a_s), _ptr(b_q), _ptr(b_e), _ptr(b_s),
+                                       _ptr(out), _dt(out), int(bool(accumulate)), _stream())
+    _check(rc, "moss_gemm_fp8_mx_grouped_dw")
+    return out
+
+
+def expert_rows(tokens, k, n_experts, multiple=32):
+    """Rows that the assignments of `tokens` tokens to k experts each take at most, each expert's filled up to `multiple`."""
+    return load().moss_expert_rows(int(tokens), int(k), int(n_experts), int(multiple))
+
+
+def expert_plan(experts, n_experts, multiple=32, rows=None):
+    """dict(row_of [T,k], source [R], offsets [n_experts + 1]) of int32 tensors for experts [T,k] int32 (numbers outside
+    [0, n_experts) are dropped); R is expert_rows(...) unless given."""
+    import torch
+    L = load()
+    assert experts.dtype == torch.int32 and experts.dim() == 2 and experts.is_contiguous()
+    dev = _same_device(experts)
+    T, k = experts.shape
+    if rows is None:
+        rows = expert_rows(T, k, n_experts, multiple)
+    i32 = torch.int32
+    plan = dict(row_of=torch.empty((T, k), dtype=i32, device=dev), source=torch.empty(max(int(rows), 0), dtype=i32, device=dev),
+                offsets=torch.empty(max(int(n_experts), 0) + 1, dtype=i32, device=dev))
+    rc = L.moss_expert_plan(_ptr(experts), T, k, int(n_experts), int(multiple), int(rows), _ptr(plan["row_of"]), _ptr(plan["source"]),
+                            _ptr(plan["offsets"]), _stream())
+    _check(rc, "moss_expert_plan")
+    return plan
+
+
+def _plan_of(plan):
+    import torch
+    row_of, source = plan["row_of"], plan["source"]
+    assert row_of.dtype == source.dtype == torch.int32 and row_of.dim() == 2 and source.dim() == 1
+    assert row_of.is_contiguous() and source.is_contiguous()
+    return row_of, source
+
+
+def _bf16_rows(t, rows, cols=None):
+    import torch
+    assert t.dtype == torch.bfloat16 and t.dim() == 2 and t.shape[0] == rows and (cols is None or t.shape[1] == cols) and t.stride(1) == 1
+
+
+def _word_out(word, device):
+    import torch
+    if word is None:
+        return torch.empty(1, dtype=torch.int32, device=device)
+    assert word.dtype == torch.int32 and word.numel() == 1 and word.device == device
+    return word
+
+
+def expert_dispatch_bf16(x, plan, y=None, absmax_bits=None):
+    """(y [R,C], max word): every token's row of x [T,C] in the rows that the plan gives it, zeros in the others."""
+    import torch
+    L = load()
+    row_of, source = _plan_of(plan)
+    T, k = row_of.shape
+    R, C_ = source.numel(), x.shape[1]
+    _bf16_rows(x, T)
+    dev = _same_device(x, row_of, source, y, absmax_bits)
+    y = _rows_out(y, R, C_, torch.bfloat16, dev)
+    _bf16_rows(y, R, C_)
+    absmax_bits = _word_out(absmax_bits, dev)
+    rc = L.moss_expert_dispatch_bf16(_ptr(x), _ptr(row_of), _ptr(source), T, k, R, C_, _ld(x), _ld(y), _ptr(y), _ptr(absmax_bits), _stream())
+    _check(rc, "moss_expert_dispatch_bf16")
+    return y, absmax_bits
+
+
+def expert_combine_bf16(y, plan, weights=None, out=None):
+    """out[t] = sum_j weights[t,j] * y[row_of[t,j]] (weights [T,k] float32; None: 1, which is the gradient of the dispatch)."""
+    import torch
+    L = load()
+    row_of, source = _plan_of(plan)
+    T, k = row_of.shape
+    R, C_ = source.numel(), y.shape[1]
+    _bf16_rows(y, R)
+    assert weights is None or (weights.dtype == torch.float32 and tuple(weights.shape) == (T, k) and weights.is_contiguous())
+    dev = _same_device(y, row_of, weights, out)
+    out = _rows_out(out, T, C_, torch.bfloat16, dev)
+    _bf16_rows(out, T, C_)
+    rc = L.moss_expert_combine_bf16(_ptr(y), _ptr(row_of), _ptr(weights), T, k, R, C_, _ld(y), _ld(out), _ptr(out), _stream())
+    _check(rc, "moss_expert_combine_bf16")
+    return out
+
+
+def expert_combine_bf16_backward(d_out, y, plan, weights, d_y=None, d_weights=None, absmax_bits=None):
+    """(d_y [R,C], d_weights [T,k], max word of d_y) for the gradient d_out [T,C] of expert_combine_bf16(y, plan, weights)."""
+    import torch
+    L = load()
+    row_of, source = _plan_of(plan)
+    T, k = row_of.shape
+    R, C_ = source.numel(), d_out.shape[1]
+    _bf16_rows(d_out, T)
+    _bf16_rows(y, R, C_)
+    assert weights.dtype == torch.float32 and tuple(weights.shape) == (T, k) and weights.is_contiguous()
+    dev = _same_device(d_out, y, row_of, source, weights, d_y, d_weights, absmax_bits)
+    if d_y is None:
+        d_y = torch.empty_strided((R, C_), (_ld(y), 1), dtype=torch.bfloat16, device=dev)
+    _bf16_rows(d_y, R, C_)
+    assert _ld(d_y) == _ld(y)
+    d_weights = _new((T, k), torch.float32, dev, d_weights)
+    absmax_bits = _word_out(absmax_bits, dev)
+    rc = L.moss_expert_combine_bf16_backward(_ptr(d_out), _ptr(y), _ptr(row_of), _ptr(source), _ptr(weights), T, k, R, C_, _ld(d_out), _ld(y),
+                                             _ptr(d_y), _ptr(d_weights), _ptr(absmax_bits), _stream())
+    _check(rc, "moss_expert_combine_bf16_backward")
+    return d_y, d_weights, absmax_bits

@@ -11,7 +11,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 LIB = os.path.join(PKG, "libmoss_hip.so")
 CALLS = os.path.join(PKG, "_moss_calls.so")
-SOURCES = ["moss_api.hip", "moss_quant.hip", "moss_weight.hip", "moss_gemm.hip", "moss_gemm_big.hip", "moss_gemm_mid.hip", "moss_swiglu.hip", "moss_rmsnorm.hip"]
+SOURCES = ["moss_api.hip", "moss_quant.hip", "moss_weight.hip", "moss_gemm.hip", "moss_gemm_big.hip", "moss_gemm_mid.hip", "moss_swiglu.hip", "moss_rmsnorm.hip",
+           "moss_block128.hip", "moss_gemm_block.hip", "moss_gemm_grouped.hip", "moss_expert.hip"]
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-ffp-contract=off",                      # numerically specified kernels: no FMA contraction

@@ -36,6 +36,78 @@ __device__ __forceinline__ void wait_lds_and_barrier()
     asm volatile("" ::: "memory");
 }
 
+// Workgroups are dealt round-robin to the 8 XCDs: the tile of this one, so that each XCD gets a contiguous range of `total`
+__device__ __forceinline__ uint32_t xcd_range_tile(uint32_t block, uint32_t total)
+{
+    const uint32_t q = total >> 3, r = total & 7, xcd = block & 7;
+    return xcd * q + (xcd < r ? xcd : r) + (block >> 3);
+}
+
+// tile `pid` of a matrix walked in bands of 8 tile rows, column by column
+__device__ __forceinline__ void band_tile(uint32_t pid, uint32_t tiles_m, uint32_t tiles_n, int &tm, int &tn)
+{
+    constexpr uint32_t kBand = 8;
+    const uint32_t band = pid / (kBand * tiles_n), rem = pid - band * kBand * tiles_n;
+    const uint32_t here = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+    tn = __builtin_amdgcn_readfirstlane((int)(rem / here));
+    tm = __builtin_amdgcn_readfirstlane((int)(band * kBand + rem % here));
+}
+
+// Rows [first, end) of a group.  Offsets come from the device and cannot be checked ahead: whatever they are, the rows lie in [0, rows).
+__device__ __forceinline__ void group_range(const int32_t *offsets, int group, int64_t rows, int64_t &first, int64_t &end)
+{
+    const int64_t a = offsets[group], b = offsets[group + 1];
+    first = a < 0 ? 0 : a < rows ? a : rows;
+    end = b < first ? first : b < rows ? b : rows;
+}
+
+struct GroupTile {
+    int group, tm, tn;
+    int64_t first, end;
+};
+
+// The tile of workgroup `block` among those of all groups, group by group, each in tiles of BM rows of its own: false if there are
+// fewer.  Every wave counts for itself, a lane per group (64 groups at a time).
+template <int BM>
+__device__ __forceinline__ bool find_group_tile(GroupTile &t, const int32_t *offsets, int groups, int64_t rows, uint32_t tiles_n, uint32_t block)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t first = 0, end = 0;
+    auto tiles_of = [&](int g) {
+        first = end = 0;
+        if (g < groups) group_range(offsets, g, rows, first, end);
+        return (uint32_t)((end - first + BM - 1) / BM);
+    };
+    uint32_t total = 0;
+    for (int g0 = 0; g0 < groups; g0 += kWave) total += wave_sum_u32(tiles_of(g0 + lane));
+    total = (uint32_t)__builtin_amdgcn_readfirstlane((int)total) * tiles_n;
+    if ((block >> 3) >= (total >> 3) + ((block & 7) < (total & 7) ? 1 : 0)) return false;
+    const uint32_t pid = xcd_range_tile(block, total);
+    uint32_t before = 0;                              // tiles of the groups ahead
+    for (int g0 = 0; g0 < groups; g0 += kWave) {
+        const uint32_t n = tiles_of(g0 + lane);
+        uint32_t upto = n;                            // rows of tiles up to and with this lane's group
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        const uint64_t behind = __ballot(before + upto * tiles_n > pid);
+        if (behind) {
+            const int at = __ffsll((unsigned long long)behind) - 1;
+            auto of_lane = [&](uint32_t v) { return (uint32_t)__builtin_amdgcn_readlane((int)v, at); };
+            const uint32_t rows_of_tiles = of_lane(n);
+            t.group = g0 + at;
+            t.first = of_lane((uint32_t)first);
+            t.end = of_lane((uint32_t)end);
+            band_tile(pid - (before + (of_lane(upto) - rows_of_tiles) * tiles_n), rows_of_tiles, tiles_n, t.tm, t.tn);
+            return true;
+        }
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63) * tiles_n;
+    }
+    return false;
+}
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -61,6 +133,19 @@ __device__ __forceinline__ void mfma_scaled(v16f &acc, const v8i &x, const v8i &
         asm volatile("v_mfma_scale_f32_32x32x64_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[1,1,0]"
                      : "+a"(acc) : "v"(x), "v"(y), "v"(sx), "v"(sy));
 }
+// The unscaled instruction, from zero and on top of what is there.  Independent and accumulating instructions back to back need no
+// wait states; whoever reads the result otherwise waits.
+__device__ __forceinline__ void mfma_unscaled_from_zero(v16f &d, const v8i &x, const v8i &y)
+{
+    asm volatile("v_mfma_f32_32x32x64_f8f6f4 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
+}
+__device__ __forceinline__ void mfma_unscaled(v16f &d, const v8i &x, const v8i &y)
+{
+    asm volatile("v_mfma_f32_32x32x64_f8f6f4 %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));
+}
+// The product of a block's two scales, kept finite so that a block of zeros adds nothing whatever they are
+__device__ __forceinline__ float block_scales(float a, float b) { return __builtin_amdgcn_fmed3f(a * b, 3.402823466e38f, -3.402823466e38f); }
+
 __device__ __forceinline__ void pin() { asm volatile("" ::: "memory"); }
 
 // Stores a 32 x 32 fragment of accumulators times `scale` without staging it.  Register v of lane (i32, h) is row i32, column

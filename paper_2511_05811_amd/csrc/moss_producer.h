@@ -26,4 +26,11 @@ int moss_internal_add_rmsnorm_bf16(const void *x, const void *delta, const void 
 int moss_internal_rmsnorm_bf16_backward(const void *h, const void *gamma, const void *dy, const void *d_res, float eps, int64_t rows,
                                         int64_t cols, int64_t ld, void *d_h, uint32_t *d_h_absmax_bits, void *workspace,
                                         size_t workspace_bytes, void *stream);
+int moss_internal_expert_dispatch_bf16(const void *x, const int32_t *row_of, const int32_t *source, int64_t tokens, int64_t k, int64_t rows,
+                                       int64_t cols, int64_t ld_x, int64_t ld_y, void *y, uint32_t *y_absmax_bits, void *workspace,
+                                       size_t workspace_bytes, void *stream);
+int moss_internal_expert_combine_bf16_backward(const void *d_out, const void *y, const int32_t *row_of, const int32_t *source,
+                                               const float *weights, int64_t tokens, int64_t k, int64_t rows, int64_t cols, int64_t ld_out,
+                                               int64_t ld_y, void *d_y, float *d_weights, uint32_t *d_y_absmax_bits, void *workspace,
+                                               size_t workspace_bytes, void *stream);
 }
