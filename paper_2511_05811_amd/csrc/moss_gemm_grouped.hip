@@ -4,6 +4,7 @@
 // How many rows a group has stands in device memory only.  The grid is made for the most tiles that there can be; a workgroup finds its
 // tile, or that there is none for it, from the offsets.  Kernel: the small tiles (moss_gemm_mid.h).
 #include "moss_gemm_mid.h"
+#include "moss_gemm_wide.h"
 
 namespace {
 
@@ -16,6 +17,23 @@ int check_common(int64_t rows, int64_t groups, const int32_t *offsets, int out_d
     if (out_dtype != MOSS_DT_BF16 && out_dtype != MOSS_DT_F32) return MOSS_ERR_UNSUPPORTED;
     if (accumulate && out_dtype != MOSS_DT_F32) return MOSS_ERR_UNSUPPORTED;
     return ((uintptr_t)offsets & 3) ? MOSS_ERR_ALIGN : MOSS_OK;
+}
+
+// Tiles: 0 .. 4 the small ones, then 128 x 256 and 256 x 256 of the wide kernel
+enum { kHalf = 5, kWide = 6 };
+
+int rows_kind(int64_t rows, int64_t N, int64_t K, int64_t groups, bool a_e, int64_t ld_out)
+{
+    const int64_t avg = (rows + groups - 1) / groups;
+    if (!a_e || K < 128 || N % 8 || ld_out % 8 || avg <= 128) return avg <= 32 ? 0 : avg <= 64 ? 1 : avg <= 128 ? 2 : 3;
+    return avg <= 256 ? kHalf : kWide;
+}
+
+int dw_kind(int64_t rows, int64_t M, int64_t N, int64_t groups)
+{
+    (void)groups;
+    if (rows < 128 || N % 8) return 3;
+    return M * N >= 1024 * 1024 ? kWide : kHalf;
 }
 
 }  // namespace
@@ -33,6 +51,21 @@ extern "C" int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int6
     if (K > ((int64_t)1 << 22) || ld_b > kMaxLd) return MOSS_ERR_UNSUPPORTED;
     if (!moss_aligned16(a_q) || !moss_aligned16(b_q) || !moss_aligned16(out) || ld_b % 16 || b_stride % 16) return MOSS_ERR_ALIGN;
     if (((uintptr_t)a_e & 3) || ((uintptr_t)a_s & 3) || ((uintptr_t)b_s & 3)) return MOSS_ERR_ALIGN;
+    hipStream_t st = (hipStream_t)stream;
+    const int kind = rows_kind(rows, N, K, groups, a_e != nullptr, ld_out);
+    if (kind >= kHalf) {
+        WideArgs p{};
+        p.M = rows; p.N = N; p.K = K;
+        p.a_q = a_q; p.a_x = a_e; p.a_s = a_s;
+        p.b_q = b_q; p.b_s = b_s;
+        p.pitch_a = K / kGroup;
+        p.end_a = rows * p.pitch_a;
+        p.ld_b = ld_b; p.b_stride = b_stride; p.b_s_stride = b_s_stride;
+        p.offsets = offsets; p.groups = (int)groups;
+        p.out = out; p.ld_out = ld_out; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
+        const int rc = kind == kWide ? launch_wide<kWideGroupRows, 8, 2>(p, st) : launch_wide<kWideGroupRows, 4, 3>(p, st);
+        if (rc != MOSS_ERR_UNSUPPORTED) return rc;
+    }
     MidGroupArgs p{};
     p.M = rows; p.N = N; p.K = K;
     p.a_q = a_q; p.a_e = a_e; p.a_s = a_s;
@@ -41,9 +74,7 @@ extern "C" int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int6
     p.e_dwords = K % 128 == 0;
     p.offsets = offsets; p.groups = (int)groups; p.rows = rows;
     p.ld_b = ld_b; p.b_stride = b_stride; p.b_s_stride = b_s_stride;
-    const int64_t avg = (rows + groups - 1) / groups;
-    const int kind = avg <= 32 ? 0 : avg <= 64 ? 1 : avg <= 128 ? 2 : 3;
-    return launch_mid_kind<kMidGroupRows>(kind, p, (hipStream_t)stream);
+    return launch_mid_kind<kMidGroupRows>(kind >= kHalf ? 3 : kind, p, st);
 }
 
 extern "C" int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
@@ -58,6 +89,22 @@ extern "C" int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, i
     if (rows > kMaxLd) return MOSS_ERR_UNSUPPORTED;
     if (!moss_aligned16(a_q) || !moss_aligned16(b_q) || !moss_aligned16(out)) return MOSS_ERR_ALIGN;
     if (((uintptr_t)a_e & 3) || ((uintptr_t)a_s & 3) || ((uintptr_t)b_e & 3) || ((uintptr_t)b_s & 3)) return MOSS_ERR_ALIGN;
+    hipStream_t st = (hipStream_t)stream;
+    const int kind = dw_kind(rows, M, N, groups);
+    if (kind >= kHalf) {
+        WideArgs p{};
+        p.M = M; p.N = N; p.K = rows;
+        p.a_q = a_q; p.a_x = a_e; p.a_s = a_s;
+        p.b_q = b_q; p.b_x = b_e; p.b_s = b_s;
+        p.pitch_a = p.pitch_b = rows / kGroup;
+        p.end_a = M * p.pitch_a;
+        p.end_b = N * p.pitch_b;
+        p.ld_b = rows;
+        p.offsets = offsets; p.groups = (int)groups;
+        p.out = out; p.ld_out = N; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
+        const int rc = kind == kWide ? launch_wide<kWideGroupDw, 8, 2>(p, st) : launch_wide<kWideGroupDw, 4, 3>(p, st);
+        if (rc != MOSS_ERR_UNSUPPORTED) return rc;
+    }
     MidGroupArgs p{};
     p.M = M; p.N = N; p.K = rows;
     p.a_q = a_q; p.a_e = a_e; p.a_s = a_s;
@@ -65,5 +112,5 @@ extern "C" int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, i
     p.out = out; p.ld_out = N; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
     p.e_dwords = rows % 128 == 0;
     p.offsets = offsets; p.groups = (int)groups; p.rows = rows;
-    return launch_mid_kind<kMidGroupDw>(3, p, (hipStream_t)stream);
+    return launch_mid_kind<kMidGroupDw>(kind >= kHalf ? 3 : kind, p, st);
 }

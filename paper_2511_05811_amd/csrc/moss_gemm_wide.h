@@ -1,0 +1,522 @@
+// Wide-tile FP8 GEMM for the products of experts and for operands with an FP32 scale per block of 128.
+//
+// Shape of the kernel
+//  * (32 MI) x 256 outputs per workgroup of 8 waves (2 x 4), two waves per SIMD, (16 MI) x 64 per wave in 16 x 16 accumulators of
+//    V_MFMA_(SCALE_)F32_16X16X128_F8F6F4, all of them vector registers: the blocked forms add to them on the vector unit.  One
+//    matrix instruction covers a stage of K = 128, which is a block.
+//  * Stages go through SLOTS slots of LDS, filled by direct global->LDS copies of 128 bytes per row.  One barrier per stage, behind the
+//    last fragment's reads of a: there the stage's slot is free, for the copies of stage + SLOTS, and the next stage has landed.  Its first fragments
+//    are read behind the last matrix instructions of this one, each b fragment behind the instruction that used its registers
+//    last.  While one wave waits its neighbour on the SIMD computes.
+//  * Blocked forms: an instruction starts from zero and leaves its sum in one of four parts.  A part is added to the accumulators
+//    times its scales when two further instructions have been issued; the matrix unit takes them one after the other, so it has
+//    retired by then.  This order is all that protects the read; the instructions are volatile asm and a part passes through an
+//    empty one at that place.
+//  * Exponents (four bytes) or scales (a float) of a stage are one dword per row.  A thread fetches those of its row for four stages ahead
+//    into registers and leaves them in a ring in LDS at the end of the four before.
+//  * Persistent workgroups walk their tiles in one stream of stages: copies and scales of the next tile are on their way while this one
+//    ends.  Three places in that stream are kept: what is computed, what is copied (SLOTS stages ahead) and what is
+//    scaled (a block of four ahead).
+//  * K that ends inside a stage, groups of rows of any length: the last stage's copies are moved back to end with the row, and what of
+//    a stage does not belong to the sum is zeroed in the fragments of a.
+//
+// Operand layout of the instruction: lane (r = lane % 16, q = lane / 16) supplies for row r the bytes K[16q, 16q + 16) in its first four
+// registers and K[64 + 16q, 64 + 16q + 16) in the last four; the 32-wide block q of row r is scaled by byte 0 of the lane's
+// scale register.  Stage layout in LDS: as in the large-tile kernel.
+#pragma once
+#include <atomic>
+#include <type_traits>
+
+#include "moss_gemm.h"
+
+namespace moss {
+
+enum WideForm { kWideGroupRows, kWideGroupDw, kWideBlock, kWideBlockRows };
+
+struct WideArgs {
+    int64_t M, N, K;                  // (kWideGroupDw: K is the length of the rows of a and b)
+    const uint8_t *a_q, *b_q;
+    const uint8_t *a_x, *b_x;         // exponents or scales (kWideGroupRows: none of b)
+    int64_t pitch_a, pitch_b;         // bytes from row to row of them
+    int64_t end_a, end_b;             // and of all
+    const float *a_s, *b_s;           // the one scale of each; of each group of b (kWideGroupRows)
+    int64_t ld_b, b_stride, b_s_stride;      // as in moss_gemm_fp8_mx_grouped (else ld_b = K)
+    const int32_t *offsets;
+    int groups;
+    void *out;
+    int64_t ld_out;
+    int out_f32, accumulate;
+    int tiles_m, tiles_n;             // (kWideGroupRows: tiles_m is not used)
+};
+
+extern __shared__ __attribute__((aligned(1024))) uint8_t wide_smem[];
+
+constexpr int kWideThreads = 512;
+constexpr int kWideBN = 256;
+constexpr int kWideK = 128;
+
+template <int MI, int SLOTS>
+struct WideShape {
+    static constexpr int kBM = 32 * MI;
+    static constexpr int kRows = kBM + kWideBN;
+    static constexpr int kSlot = kRows * kWideK;
+    static constexpr int kPieces = kRows / 8 / 8;               // 8-row copies per wave and stage
+    static constexpr int kRing = SLOTS * kSlot;                 // [2 blocks][4 stages][rows] dwords
+    static constexpr int kTable = kRing + 8 * kRows * 4;        // tiles ahead of each group (kWideGroupRows)
+    static_assert(kRows % 64 == 0 && kBM % 16 == 0, "whole copies per wave");
+    static constexpr int lds_bytes(WideForm form, int groups) { return kTable + (form == kWideGroupRows ? (groups + 1) * 4 : 0); }
+};
+
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_at1 __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t u32_at1 __attribute__((aligned(1)));
+
+__device__ __forceinline__ void mfma16_from_zero(v4f &d, const v8i &x, const v8i &y)
+{
+    asm volatile("v_mfma_f32_16x16x128_f8f6f4 %0, %1, %2, 0" : "=&v"(d) : "v"(x), "v"(y));
+}
+__device__ __forceinline__ void mfma16_scaled(v4f &d, const v8i &x, const v8i &y, uint32_t sx, uint32_t sy)
+{
+    asm volatile("v_mfma_scale_f32_16x16x128_f8f6f4 %0, %1, %2, %0, %3, %4 op_sel_hi:[0,0,0]" : "+v"(d) : "v"(x), "v"(y), "v"(sx), "v"(sy));
+}
+
+// Stores the 16 x 32 outputs of two fragments side by side.  Lane (r, q) holds row r, columns 4 q .. 4 q + 3 of each.  BF16: lanes of
+// neighbouring q exchange a fragment each and hold eight columns of one.  (N and ld are multiples of 8: pieces are whole)
+__device__ __forceinline__ void store_pair(const v4f &x, const v4f &y, float scale, void *out, int64_t ld, int64_t row, int64_t n, int q, int64_t M,
+                                           int64_t N, int out_f32, int accumulate)
+{
+    if (out_f32) {
+#pragma unroll
+        for (int f = 0; f < 2; f++) {
+            const v4f &d = f ? y : x;
+            const int64_t at = n + 16 * f + 4 * q;
+            if (row >= M || at >= N) continue;
+            float *o = reinterpret_cast<float *>(out) + row * ld + at;
+            float4 v = make_float4(d[0] * scale, d[1] * scale, d[2] * scale, d[3] * scale);
+            if (accumulate) {
+                const float4 old = *reinterpret_cast<const float4 *>(o);
+                v.x += old.x; v.y += old.y; v.z += old.z; v.w += old.w;
+            }
+            *reinterpret_cast<float4 *>(o) = v;
+        }
+        return;
+    }
+    uint32_t w[4] = {pack_bf16(x[0] * scale, x[1] * scale), pack_bf16(x[2] * scale, x[3] * scale), pack_bf16(y[0] * scale, y[1] * scale),
+                     pack_bf16(y[2] * scale, y[3] * scale)};
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const auto both = __builtin_amdgcn_permlane16_swap(w[k], w[2 + k], false, false);
+        w[k] = both[0];
+        w[2 + k] = both[1];
+    }
+    // q even: columns 4 q .. 4 q + 7 of the first fragment, odd: 4 (q - 1) .. of the second
+    const int64_t at = n + 16 * (q & 1) + 4 * (q & 2);
+    if (row < M && at < N) *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(out) + row * ld + at) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Row tiles of the groups ahead of each, [groups + 1], by the first wave
+template <int BM>
+__device__ __forceinline__ void count_group_tiles(uint32_t *table, const int32_t *offsets, int groups, int64_t rows)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (int g0 = 0; g0 < groups; g0 += kWave) {
+        uint32_t n = 0;
+        if (g0 + lane < groups) {
+            int64_t first, end;
+            group_range(offsets, g0 + lane, rows, first, end);
+            n = (uint32_t)((end - first + BM - 1) / BM);
+        }
+        uint32_t upto = n;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        if (g0 + lane < groups) table[g0 + lane] = before + upto - n;
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+    if (lane == 0) table[groups] = before;
+}
+
+template <WideForm FORM, int MI, int SLOTS>
+__global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
+{
+    using S = WideShape<MI, SLOTS>;
+    constexpr bool kBlocked = FORM == kWideBlock || FORM == kWideBlockRows;
+    constexpr int kBM = S::kBM, kPieces = S::kPieces;
+    const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)wide_smem;
+    uint32_t *ring = reinterpret_cast<uint32_t *>(wide_smem + S::kRing), *table = reinterpret_cast<uint32_t *>(wide_smem + S::kTable);
+    const int64_t ld_a = p.K;
+
+    uint32_t total;
+    if constexpr (FORM == kWideGroupRows) {
+        if (wave == 0) count_group_tiles<kBM>(table, p.offsets, p.groups, p.M);
+        __syncthreads();
+        total = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[p.groups]) * (uint32_t)p.tiles_n;
+    } else {
+        total = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n * (FORM == kWideGroupDw ? (uint32_t)p.groups : 1u);
+    }
+    if (blockIdx.x >= total) return;
+    const int n_tiles = (int)((total - blockIdx.x + gridDim.x - 1) / gridDim.x);
+
+    // Tile k of this workgroup: each XCD gets a contiguous range (gridDim.x is a multiple of 8 if a workgroup has more than one), in
+    // bands of 4 tile rows
+    struct Tile {
+        int64_t m0, n0, rows_end, first, end;        // rows of a below rows_end; the sum is over [first, end)
+        int group, T;
+    };
+    auto tile_of = [&](int k) {
+        Tile t;
+        const uint32_t pid = blockIdx.x + (uint32_t)k * gridDim.x;
+        const uint32_t each8 = total >> 3, left = total & 7, xcd = pid & 7;
+        uint32_t at = xcd * each8 + (xcd < left ? xcd : left) + (pid >> 3);
+        uint32_t tiles_m = (uint32_t)p.tiles_m;
+        t.group = 0;
+        t.m0 = 0;
+        t.rows_end = p.M;
+        t.first = 0;
+        t.end = p.K;
+        if constexpr (FORM == kWideGroupRows) {
+            int g = 0;
+            for (int g0 = 0; g0 < p.groups; g0 += kWave) {       // groups that start at or ahead of this tile
+                const int o = g0 + lane;
+                g += __popcll(__ballot(o < p.groups && table[o < p.groups ? o : p.groups] * (uint32_t)p.tiles_n <= at));
+            }
+            t.group = __builtin_amdgcn_readfirstlane(g - 1);
+            const uint32_t ahead = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group]);
+            tiles_m = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group + 1]) - ahead;
+            at -= ahead * (uint32_t)p.tiles_n;
+            group_range(p.offsets, t.group, p.M, t.m0, t.rows_end);
+        }
+        if constexpr (FORM == kWideGroupDw) {
+            const uint32_t each = tiles_m * (uint32_t)p.tiles_n;
+            t.group = __builtin_amdgcn_readfirstlane((int)(at / each));
+            at -= (uint32_t)t.group * each;
+            group_range(p.offsets, t.group, p.K, t.first, t.end);
+            t.first &= ~(int64_t)(kGroup - 1);                   // (they are multiples of 32 already, by contract)
+            t.end &= ~(int64_t)(kGroup - 1);
+        }
+        constexpr uint32_t kBand = 4;
+        const uint32_t band = at / (kBand * (uint32_t)p.tiles_n), rem = at - band * kBand * (uint32_t)p.tiles_n;
+        const uint32_t here = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
+        t.n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / here)) * kWideBN;
+        t.m0 += (int64_t)__builtin_amdgcn_readfirstlane((int)(band * kBand + rem % here)) * kBM;
+        t.T = (int)((t.end - t.first + kWideK - 1) / kWideK);
+        if (t.T == 0) t.T = 1;                                   // (nothing to add, but zeros to store)
+        return t;
+    };
+    // first byte of stage P of a row: moved back where the row would end inside it
+    auto stage_at = [&](const Tile &t, int P) {
+        const int64_t at = t.first + (int64_t)P * kWideK, last = p.K - kWideK;
+        return at < last ? at : last;
+    };
+
+    // ---- what is copied
+    const int piece0 = wave * kPieces;
+    int c_tile = 0, c_P = 0;
+    Tile ct = tile_of(0);
+    const uint8_t *ca, *cb;
+    int c_last_a, c_last_b;
+    auto copy_tile = [&]() {
+        ca = p.a_q + ct.m0 * ld_a;
+        cb = p.b_q + ct.n0 * p.ld_b + (FORM == kWideGroupRows ? ct.group * p.b_stride : 0);
+        c_last_a = (int)(ct.rows_end - ct.m0 < kBM ? ct.rows_end - ct.m0 : kBM) - 1;
+        c_last_b = (int)(p.N - ct.n0 < kWideBN ? p.N - ct.n0 : kWideBN) - 1;
+    };
+    uint32_t c_slot = 0;
+    const uint8_t *sa_ptr, *sb_ptr;                  // of the stage to copy
+    auto copy_begin = [&]() {
+        const int64_t at = stage_at(ct, c_P);
+        sa_ptr = ca + at;
+        sb_ptr = cb + at;
+    };
+    // 8 rows of a or of b; rows beyond the matrix repeat the last.  (The lane's offset is worked out anew: there are no registers for
+    // those of all pieces.)
+    auto copy_piece = [&](int x) {
+        const bool is_a = piece0 + x < kBM / 8;
+        const int r = (piece0 + x - (is_a ? 0 : kBM / 8)) * 8 + (lane >> 3), last = is_a ? c_last_a : c_last_b;
+        const uint32_t chunk = (uint32_t)((lane & 7) ^ ((r >> 1) & 7)) * 16;
+        const uint32_t off = (uint32_t)(r < last ? r : last) * (uint32_t)(is_a ? ld_a : p.ld_b) + chunk;
+        dma16_at(is_a ? sa_ptr : sb_ptr, off, lds0 + c_slot + (uint32_t)piece0 * 1024, x * 1024);
+    };
+    auto copy_end = [&]() {
+        c_slot = c_slot + S::kSlot == SLOTS * S::kSlot ? 0 : c_slot + S::kSlot;
+        if (++c_P == ct.T) {
+            c_P = 0;
+            if (++c_tile < n_tiles) {
+                ct = tile_of(c_tile);
+                copy_tile();
+            }
+        }
+    };
+
+    // ---- what is scaled: this thread's row, four dwords at a time
+    int s_tile = 0, s_block = 0, s_blocks = 1, s_T = 1;
+    const bool s_is_a = wave < kBM / kWave, s_there = wave < S::kRows / kWave && (FORM != kWideGroupRows || s_is_a);
+    const uint8_t *s_base = nullptr;                 // of the tile's first row
+    uint32_t s_row = 0, s_end = 0;                   // bytes from there: this row, the end of the array (no row of the tile is 4 GB away)
+    uint32_t s_back = 0;                             // exponents by which the tile's last stage is moved back
+    uint32_t words[4];
+    int moved = 4;                                   // the one of them that is moved by so many exponents
+    uint32_t moved_by = 0;
+    auto scale_tile = [&](const Tile &t) {
+        s_blocks = (t.T + 3) >> 2;
+        s_T = t.T;
+        // (from where the first stage is copied, at least four exponents ahead of the row's end)
+        const int64_t begin = stage_at(t, 0);
+        if (!kBlocked) s_back = (uint32_t)((begin + (int64_t)(t.T - 1) * kWideK - stage_at(t, t.T - 1)) >> 5);
+        if (!s_there) return;
+        const int64_t row0 = s_is_a ? t.m0 : FORM == kWideBlock ? t.n0 >> 7 : t.n0, pitch = s_is_a ? p.pitch_a : p.pitch_b;
+        const int last = (int)((s_is_a ? t.rows_end - t.m0 : p.N - t.n0) < 256 ? (s_is_a ? t.rows_end - t.m0 : p.N - t.n0) : 256) - 1;
+        int r = s_is_a ? tid : tid - kBM;
+        r = r < last ? r : last;
+        if (FORM == kWideBlock && !s_is_a) r >>= 7;
+        const int64_t skip = row0 * pitch + (FORM == kWideGroupDw ? begin >> 5 : 0), left = (s_is_a ? p.end_a : p.end_b) - skip;
+        s_base = (s_is_a ? p.a_x : p.b_x) + skip;
+        s_end = left < 0xFFFFFFFFll ? (uint32_t)left : 0xFFFFFFFFu;
+        s_row = (uint32_t)r * (uint32_t)pitch;
+    };
+    auto scale_load = [&]() {
+        if (s_there) {
+            const uint32_t at = s_row + (uint32_t)s_block * 16;
+            if (at + 16 <= s_end) {
+                const u32x4_at1 v = *reinterpret_cast<const u32x4_at1 *>(s_base + at);
+                words[0] = v.x; words[1] = v.y; words[2] = v.z; words[3] = v.w;
+            } else {
+                // the array ends here: its last four bytes, moved to their place in the word
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    const uint32_t w = at + 4 * u, from = w + 4 <= s_end ? w : s_end - 4;
+                    words[u] = *reinterpret_cast<const u32_at1 *>(s_base + from) >> (8 * ((w - from) & 3));
+                }
+            }
+        }
+        if (!kBlocked) {
+            moved = s_block == s_blocks - 1 ? (s_T - 1) & 3 : 4;
+            moved_by = 8 * s_back;
+        }
+        if (++s_block == s_blocks) {
+            s_block = 0;
+            if (++s_tile < n_tiles) scale_tile(tile_of(s_tile));
+        }
+    };
+    auto scale_store = [&](int half) {
+        if (s_there)
+#pragma unroll
+            for (int u = 0; u < 4; u++) ring[(half * 4 + u) * S::kRows + tid] = !kBlocked && u == moved ? words[u] << moved_by : words[u];
+    };
+
+    // ---- what is computed
+    v4f acc[MI][4], part[kBlocked ? 4 : 1];
+    v8i fa[2], fb[4];
+    uint32_t sa[4] = {0, 0, 0, 0}, sb[4];            // exponent bytes (sb: of each fragment); scales of rows of a, of blocks of b
+    float row_scale[FORM == kWideBlockRows ? 4 : 1][4], both[2];
+    const int sw = (r16 >> 1) & 7;
+    const uint32_t lane_at = (uint32_t)(r16 * kWideK + ((q ^ sw) << 4));
+    const uint32_t a_at = lane_at + (uint32_t)(wm * 16 * MI * kWideK), b_at = lane_at + (uint32_t)((kBM + wn * 64) * kWideK);
+    // (chunk q + 4 of a row lies 64 bytes from chunk q, whichever way)
+    auto read_fragment = [&](v8i &f, uint32_t at, uint32_t at64) {
+        const uint4 lo = *reinterpret_cast<const uint4 *>(wide_smem + at), hi = *reinterpret_cast<const uint4 *>(wide_smem + at64);
+        f[0] = (int)lo.x; f[1] = (int)lo.y; f[2] = (int)lo.z; f[3] = (int)lo.w;
+        f[4] = (int)hi.x; f[5] = (int)hi.y; f[6] = (int)hi.z; f[7] = (int)hi.w;
+    };
+    auto read_a = [&](int i, uint32_t slot, int stage) {
+        read_fragment(fa[i & 1], a_at + slot + (uint32_t)(i * 16 * kWideK), (a_at ^ 64) + slot + (uint32_t)(i * 16 * kWideK));
+        const uint32_t *x = ring + stage * S::kRows + wm * 16 * MI + i * 16 + r16;
+        sa[i & 3] = kBlocked ? *x : (uint32_t)reinterpret_cast<const uint8_t *>(x)[q];
+    };
+    auto read_b = [&](int j, uint32_t slot) { read_fragment(fb[j], b_at + slot + (uint32_t)(j * 16 * kWideK), (b_at ^ 64) + slot + (uint32_t)(j * 16 * kWideK)); };
+    auto read_b_scale = [&](int j, int stage) {
+        const uint32_t *x = ring + stage * S::kRows + kBM + wn * 64 + j * 16;
+        if (FORM == kWideBlock) {
+            if (j == 0) sb[0] = x[0];                            // (64 columns share it)
+        } else if (FORM == kWideBlockRows) {
+            const float4 v = *reinterpret_cast<const float4 *>(x + 4 * q);
+            row_scale[FORM == kWideBlockRows ? j : 0][0] = v.x; row_scale[FORM == kWideBlockRows ? j : 0][1] = v.y;
+            row_scale[FORM == kWideBlockRows ? j : 0][2] = v.z; row_scale[FORM == kWideBlockRows ? j : 0][3] = v.w;
+        } else if (FORM == kWideGroupDw) {
+            sb[j] = (uint32_t)reinterpret_cast<const uint8_t *>(x + r16)[q];
+        } else {
+            sb[j] = 127;
+        }
+    };
+    auto fold = [&](int i, int j) {
+        v4f &d = part[kBlocked ? j : 0];
+        asm volatile("" : "+v"(d));
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+            if (FORM == kWideBlockRows) acc[i][j][v] = __builtin_fmaf(d[v] * __uint_as_float(sa[i & 3]), row_scale[FORM == kWideBlockRows ? j : 0][v], acc[i][j][v]);
+            else acc[i][j][v] = __builtin_fmaf(d[v], both[i & 1], acc[i][j][v]);
+        }
+        asm volatile("" : "+v"(acc[i][j]));          // (here, and not when the part's registers are needed again)
+    };
+
+    // ---- the first stages
+    copy_tile();
+#pragma unroll
+    for (int s = 0; s < SLOTS; s++)
+        if (c_tile < n_tiles) {
+            copy_begin();
+#pragma unroll
+            for (int x = 0; x < kPieces; x++) copy_piece(x);
+            copy_end();
+        }
+    scale_tile(tile_of(0));
+    scale_load();
+    scale_store(0);
+    wait_vmcnt<0>();
+    wait_lds_and_barrier();
+    int half = 0;
+    uint32_t slot = 0;
+    read_a(0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < 4; j++) {
+        read_b(j, 0);
+        read_b_scale(j, 0);
+    }
+
+    for (int k = 0; k < n_tiles; k++) {
+        const Tile t = tile_of(k);
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) acc[i][j][v] = 0.0f;
+        if (kBlocked) {
+            // what the first instructions fold is nothing
+            both[1] = 0.0f;
+#pragma unroll
+            for (int j = 2; j < 4; j++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) part[kBlocked ? j : 0][v] = 0.0f;
+        }
+        for (int P = 0; P < t.T; P++) {
+            const bool block_ends = (P & 3) == 3 || P == t.T - 1;
+            if ((P & 3) == 0 && s_tile < n_tiles) scale_load();
+            const int stage = half * 4 + (P & 3), next_stage = block_ends ? (half ^ 1) * 4 : stage + 1;
+            const uint32_t next_slot = slot + S::kSlot == SLOTS * S::kSlot ? 0 : slot + S::kSlot;
+            // 16-byte chunks of this stage that belong to the sum
+            const int64_t at = stage_at(t, P), from = t.first + (int64_t)P * kWideK;
+            const int64_t to = t.end < from + kWideK ? t.end : from + kWideK;
+            const int lo = (int)((from - at) >> 4), hi = (int)((to - at) >> 4);
+            const bool whole = lo == 0 && hi == 8;
+            bool copies = false;
+#pragma unroll
+            for (int i = 0; i < MI; i++) {
+                if (!whole) {
+#pragma unroll
+                    for (int v = 0; v < 8; v++) {
+                        const int c = q + (v < 4 ? 0 : 4);
+                        if (c < lo || c >= hi) fa[i & 1][v] = 0;
+                    }
+                    asm volatile("s_nop 4" : "+v"(fa[i & 1]));   // vector ALU write -> operand of a matrix instruction
+                }
+                if (!kBlocked) {
+                    // vector ALU write (the byte of the exponent) -> operand of a matrix instruction
+                    if (i == 0) asm volatile("" : "+v"(sb[0]), "+v"(sb[1]), "+v"(sb[2]), "+v"(sb[3]));
+                    asm volatile("s_nop 4" : "+v"(sa[i & 3]));
+                }
+                if (FORM == kWideBlock) both[i & 1] = block_scales(__uint_as_float(sa[i & 3]), __uint_as_float(sb[0]));
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    if (kBlocked) mfma16_from_zero(part[kBlocked ? j : 0], fb[j], fa[i & 1]);
+                    else mfma16_scaled(acc[i][j], fb[j], fa[i & 1], sb[j], sa[i & 3]);
+                    if (kBlocked) {
+                        if (j >= 2) {
+                            fold(i, j - 2);
+                            if (i == MI - 1 && FORM == kWideBlockRows) read_b_scale(j - 2, next_stage);
+                        } else {
+                            fold((i + MI - 1) % MI, j + 2);
+                            if (i == 0 && FORM == kWideBlockRows) read_b_scale(j + 2, stage);
+                        }
+                    }
+                    if (i + 1 < MI && j == 0) read_a(i + 1, slot, stage);
+                    if (i == MI - 1) {
+                        if (j == 0) read_a(0, next_slot, next_stage);
+                        read_b(j, next_slot);
+                        if (FORM != kWideBlockRows) read_b_scale(j, next_stage);
+                        if (copies)
+#pragma unroll
+                            for (int x = j * kPieces / 4; x < (j + 1) * kPieces / 4; x++) copy_piece(x);
+                    }
+                    pin();
+                }
+                if (i == MI - 2) {
+                    // every wave has read this stage, and the next has landed
+                    copies = c_tile < n_tiles;
+                    if (SLOTS > 2 && copies) wait_vmcnt<(SLOTS - 2) * kPieces>();
+                    else wait_vmcnt<0>();
+                    if (block_ends) scale_store(half ^ 1);
+                    wait_lds_and_barrier();
+                    if (copies) copy_begin();
+                }
+            }
+            if (copies) copy_end();
+            if (block_ends) half ^= 1;
+            slot = next_slot;
+        }
+        // ---- epilogue: straight from the registers
+        float scale = 1.0f;
+        if (kBlocked) {
+            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last matrix instructions retire
+            fold(MI - 1, 2);
+            fold(MI - 1, 3);
+        } else {
+            scale = *p.a_s * p.b_s[FORM == kWideGroupRows ? t.group * p.b_s_stride : 0];
+            asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < MI; i++)
+#pragma unroll
+                for (int j = 0; j < 4; j++) asm volatile("" : "+v"(acc[i][j]));
+        }
+        void *out = p.out;
+        if (FORM == kWideGroupDw) out = (uint8_t *)p.out + (int64_t)t.group * p.M * p.ld_out * (p.out_f32 ? 4 : 2);
+#pragma unroll
+        for (int i = 0; i < MI; i++)
+#pragma unroll
+            for (int j = 0; j < 4; j += 2)
+                store_pair(acc[i][j], acc[i][j + 1], scale, out, p.ld_out, t.m0 + wm * 16 * MI + i * 16 + r16, t.n0 + wn * 64 + j * 16, q, t.rows_end, p.N,
+                           p.out_f32, p.accumulate);
+    }
+    wait_vmcnt<0>();   // no copy into LDS may be outstanding when the wave ends
+}
+
+template <WideForm FORM, int MI, int SLOTS>
+static int launch_wide(WideArgs p, hipStream_t st)
+{
+    using S = WideShape<MI, SLOTS>;
+    int cus = moss_internal_cu_count();
+    cus = cus <= 0 ? 256 : cus >= 8 ? cus & ~7 : 8;
+    const int64_t tiles_n = (p.N + kWideBN - 1) / kWideBN;
+    int64_t tiles_m = (p.M + S::kBM - 1) / S::kBM, total = tiles_m * tiles_n;
+    int64_t most = total;
+    if (FORM == kWideGroupRows) {
+        const int64_t some = p.groups < p.M ? p.groups : p.M;
+        total = (p.M + some * (S::kBM - 1)) / S::kBM * tiles_n;
+        most = tiles_m * p.groups * tiles_n;         // whatever the offsets are
+    }
+    if (FORM == kWideGroupDw) most = total *= p.groups;
+    if (most > 0x7FFFFFF) return MOSS_ERR_UNSUPPORTED;
+    p.tiles_m = (int)tiles_m;
+    p.tiles_n = (int)tiles_n;
+    const auto kern = k_gemm_wide<FORM, MI, SLOTS>;
+    static std::atomic<bool> attr_set[64];           // per device: the LDS size it may ask for has been raised
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOSS_ERR_HIP;
+    if (!attr_set[dev].load()) {
+        if (hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) {
+            (void)hipGetLastError();
+            return MOSS_ERR_UNSUPPORTED;
+        }
+        attr_set[dev].store(true);
+    }
+    hipLaunchKernelGGL(kern, dim3((unsigned)(total < cus ? total : cus)), dim3(kWideThreads), (size_t)S::lds_bytes(FORM, p.groups), st, p);
+    if (hipGetLastError() != hipSuccess) return MOSS_ERR_HIP;
+    return MOSS_OK;
+}
+
+}  // namespace moss

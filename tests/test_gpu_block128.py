@@ -126,6 +126,22 @@ def test_products_at_every_edge(M, N, K, b_block):
     assert bool((wide[:, N:] == 7.0).all())
 
 
+# large tiles: whole and ragged K, edges inside a fragment, a tile of one row, more tiles than compute units
+@pytest.mark.parametrize("M,N,K", [(600, 520, 128), (513, 1032, 160), (1, 300000, 256), (2050, 4104, 288), (300, 1000, 8224), (4353, 4096, 640), (2048, 4096, 1024)])
+@pytest.mark.parametrize("b_block", [1, 128])
+def test_products_in_large_tiles(M, N, K, b_block):
+    a, a_s, b, b_s = operands(M, N, K, b_block, M + N + K)
+    A, B = values(a, a_s, 1), values(b, b_s, b_block)
+    d = [to_gpu(t) for t in (a, a_s, b, b_s)]
+    check_product(moss.gemm_fp8_block128(*d), A, B)
+    wide = torch.full((M, N + 8), 7.0, device=dev())
+    out = moss.gemm_fp8_block128(*d, out=wide[:, :N])
+    check_product(out, A, B)
+    base = out.double().cpu().numpy()
+    check_product(moss.gemm_fp8_block128(*d, out=wide[:, :N], accumulate=True), A, B, base)
+    assert bool((wide[:, N:] == 7.0).all())
+
+
 def test_blocks_of_zeros_and_scales_of_any_size():
     """A block that is all zeros adds nothing whatever its scale; scales from 2^-100 to 2^100 keep their products."""
     M, N, K = 70, 90, 640
