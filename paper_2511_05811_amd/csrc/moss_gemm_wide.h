@@ -114,6 +114,18 @@ __device__ __forceinline__ void store_pair(const v4f &x, const v4f &y, float sca
     if (row < M && at < N) *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(out) + row * ld + at) = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Weight gradients of groups of any length: an XCD gets an eighth of every group's tiles (side by side, for the L2), the eighths in
+// turn, so that all have the same share of long and short sums.  (Whole groups side by side: 8 groups of 4096 x 4096 whose lengths
+// differ by a factor of five kept the XCD of the longest for 709 us.)  Tiles of group g in the list of XCD x, and of the first n groups.
+__host__ __device__ __forceinline__ uint32_t eighth_begin(uint32_t each, uint32_t part) { return (uint32_t)((uint64_t)each * part >> 3); }
+__host__ __device__ __forceinline__ uint32_t eighth_size(uint32_t each, uint32_t part) { return eighth_begin(each, part + 1) - eighth_begin(each, part); }
+__host__ __device__ __forceinline__ uint32_t eighths_of(uint32_t each, uint32_t xcd, uint32_t groups)
+{
+    uint32_t n = (groups >> 3) * each;               // (eight groups in a row give every part once)
+    for (uint32_t g = groups & ~7u; g < groups; g++) n += eighth_size(each, (xcd + g) & 7);
+    return n;
+}
+
 // Row tiles of the groups ahead of each, [groups + 1], by the first wave
 template <int BM>
 __device__ __forceinline__ void count_group_tiles(uint32_t *table, const int32_t *offsets, int groups, int64_t rows)
@@ -151,28 +163,37 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     uint32_t *ring = reinterpret_cast<uint32_t *>(wide_smem + S::kRing), *table = reinterpret_cast<uint32_t *>(wide_smem + S::kTable);
     const int64_t ld_a = p.K;
 
-    uint32_t total;
+    // (workgroups are dealt round-robin to the XCDs; gridDim.x is a multiple of 8 if one of them has more than one tile)
+    const uint32_t each = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n, xcd = blockIdx.x & 7;
+    uint32_t total = each, mine = blockIdx.x, step = gridDim.x;
     if constexpr (FORM == kWideGroupRows) {
         if (wave == 0) count_group_tiles<kBM>(table, p.offsets, p.groups, p.M);
         __syncthreads();
         total = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[p.groups]) * (uint32_t)p.tiles_n;
-    } else {
-        total = (uint32_t)p.tiles_m * (uint32_t)p.tiles_n * (FORM == kWideGroupDw ? (uint32_t)p.groups : 1u);
     }
-    if (blockIdx.x >= total) return;
-    const int n_tiles = (int)((total - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    if constexpr (FORM == kWideGroupDw) {
+        total = eighths_of(each, xcd, (uint32_t)p.groups);
+        mine >>= 3;
+        step >>= 3;
+    }
+    if (mine >= total) return;
+    const int n_tiles = (int)((total - mine + step - 1) / step);
 
-    // Tile k of this workgroup: each XCD gets a contiguous range (gridDim.x is a multiple of 8 if a workgroup has more than one), in
-    // bands of 4 tile rows
+    // Tile k of this workgroup, in bands of 4 tile rows; each XCD gets a contiguous range, or its part of every group
     struct Tile {
         int64_t m0, n0, rows_end, first, end;        // rows of a below rows_end; the sum is over [first, end)
         int group, T;
     };
     auto tile_of = [&](int k) {
         Tile t;
-        const uint32_t pid = blockIdx.x + (uint32_t)k * gridDim.x;
-        const uint32_t each8 = total >> 3, left = total & 7, xcd = pid & 7;
-        uint32_t at = xcd * each8 + (xcd < left ? xcd : left) + (pid >> 3);
+        const uint32_t pid = mine + (uint32_t)k * step;
+        uint32_t at = pid;
+        if constexpr (FORM != kWideGroupDw) {
+            at = xcd_range_tile(pid, total);
+        } else {
+            at += xcd * (total >> 3);                // (each begins elsewhere in its list)
+            if (at >= total) at -= total;
+        }
         uint32_t tiles_m = (uint32_t)p.tiles_m;
         t.group = 0;
         t.m0 = 0;
@@ -192,9 +213,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
             group_range(p.offsets, t.group, p.M, t.m0, t.rows_end);
         }
         if constexpr (FORM == kWideGroupDw) {
-            const uint32_t each = tiles_m * (uint32_t)p.tiles_n;
-            t.group = __builtin_amdgcn_readfirstlane((int)(at / each));
-            at -= (uint32_t)t.group * each;
+            uint32_t g = __builtin_amdgcn_readfirstlane((int)(at / each)) * 8;
+            at -= (g >> 3) * each;
+            for (uint32_t n; at >= (n = eighth_size(each, (xcd + g) & 7)); g++) at -= n;
+            at += eighth_begin(each, (xcd + g) & 7);
+            t.group = (int)g;
             group_range(p.offsets, t.group, p.K, t.first, t.end);
             t.first &= ~(int64_t)(kGroup - 1);                   // (they are multiples of 32 already, by contract)
             t.end &= ~(int64_t)(kGroup - 1);
@@ -499,8 +522,16 @@ static int launch_wide(WideArgs p, hipStream_t st)
         total = (p.M + some * (S::kBM - 1)) / S::kBM * tiles_n;
         most = tiles_m * p.groups * tiles_n;         // whatever the offsets are
     }
-    if (FORM == kWideGroupDw) most = total *= p.groups;
+    if (FORM == kWideGroupDw) most = total * p.groups;
     if (most > 0x7FFFFFF) return MOSS_ERR_UNSUPPORTED;
+    if (FORM == kWideGroupDw) {
+        uint32_t longest = 0;
+        for (uint32_t x = 0; x < 8; x++) {
+            const uint32_t n = eighths_of((uint32_t)total, x, (uint32_t)p.groups);
+            longest = n > longest ? n : longest;
+        }
+        total = 8 * (int64_t)longest;
+    }
     p.tiles_m = (int)tiles_m;
     p.tiles_n = (int)tiles_n;
     const auto kern = k_gemm_wide<FORM, MI, SLOTS>;
