@@ -110,7 +110,9 @@ def _bind_calls():
     import torch
     names = ("moss_quant_workspace_bytes", "moss_quant_act_2level", "moss_quant_act_2level_given_max", "moss_gemm_fp8_mx",
              "moss_weight_workspace_bytes", "moss_weight_autoscale_cast", "moss_internal_swiglu_bf16", "moss_internal_swiglu_bf16_backward",
-             "moss_internal_add_rmsnorm_bf16", "moss_internal_rmsnorm_bf16_backward")     # (these take scratch)
+             "moss_internal_add_rmsnorm_bf16", "moss_internal_rmsnorm_bf16_backward",     # (these take scratch)
+             "moss_quant_block128", "moss_gemm_fp8_block128", "moss_gemm_fp8_mx_grouped", "moss_gemm_fp8_mx_grouped_dw", "moss_expert_rows",
+             "moss_expert_plan", "moss_internal_expert_dispatch_bf16", "moss_expert_combine_bf16", "moss_internal_expert_combine_bf16_backward")
     try:
         from . import _moss_calls as native
         get_device, get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
@@ -477,6 +479,11 @@ def _ld(t):
 def quant_block128(x, flags=MOSS_Q_ROW, out=None):
     """Groups of 128 with an FP32 scale each; x: torch.bfloat16 [rows, cols] on the GPU (row stride may exceed cols).
     Returns dict(q_row, s_row, q_col, s_col) of device tensors (absent outputs are None)."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.quant_block128(x, flags, out)
+        if done is not None:
+            return done
     import torch
     L = load()
     assert x.dtype == torch.bfloat16 and x.dim() == 2 and x.stride(1) == 1
@@ -519,6 +526,11 @@ def quant_block128_weight(w, want_transpose=False, wq=None, s=None, wq_t=None, s
 def gemm_fp8_block128(a_q, a_s, b_q, b_s, out=None, out_dtype=None, accumulate=False):
     """out[m,n] (+)= sum over blocks of 128 of k of a_s[m,block] b_s[n or n // 128,block] * sum a[m,k] b[n,k]; a_q [M,K], b_q [N,K]
     uint8, a_s [M,ceil(K/128)], b_s [ceil(N/128),ceil(K/128)] (a weight) or [N,ceil(K/128)], float32, all dense."""
+    native = _bind_calls() if _calls is None else _calls
+    if native and (out_dtype is None or out is not None):
+        done = native.gemm_fp8_block128(a_q, a_s, b_q, b_s, out, accumulate)
+        if done is not None:
+            return done
     import torch
     L = load()
     M, K = a_q.shape
@@ -539,6 +551,11 @@ def gemm_fp8_mx_grouped(a_q, a_e, a_s, b_q, b_s, offsets, out=None, out_dtype=No
     """Row r of group g (offsets[g] <= r < offsets[g + 1], int32): out[r,n] (+)= a_s*b_s[g]*sum_k a[r,k] 2^(ae-127) b[g,n,k]; a_q [R,K],
     a_e [R,K/32] or None, a_s a float32 scalar, b_q [G,N,K] (neighbours along K; other strides multiples of 16), b_s [G] float32 of any
     stride, or one scale for all.  Rows of no group stay as they were."""
+    native = _bind_calls() if _calls is None else _calls
+    if native and (out_dtype is None or out is not None):
+        done = native.gemm_fp8_mx_grouped(a_q, a_e, a_s, b_q, b_s, offsets, out, accumulate)
+        if done is not None:
+            return done
     import torch
     L = load()
     R, K = a_q.shape
@@ -559,6 +576,11 @@ def gemm_fp8_mx_grouped(a_q, a_e, a_s, b_q, b_s, offsets, out=None, out_dtype=No
 def gemm_fp8_mx_grouped_dw(a_q, a_e, a_s, b_q, b_e, b_s, offsets, out=None, out_dtype=None, accumulate=False):
     """out[g,m,n] (+)= a_s*b_s*sum over r of group g (offsets as above, multiples of 32) of a[m,r] 2^(ae-127) b[n,r] 2^(be-127); a_q [M,R],
     b_q [N,R] uint8, a_e/b_e uint8 [.,R/32], a_s/b_s float32 scalars.  Without `out` a float32 tensor [G,M,N]."""
+    native = _bind_calls() if _calls is None else _calls
+    if native and (out_dtype is None or out is not None):
+        done = native.gemm_fp8_mx_grouped_dw(a_q, a_e, a_s, b_q, b_e, b_s, offsets, out, accumulate)
+        if done is not None:
+            return done
     import torch
     L = load()
     M, R = a_q.shape
@@ -585,6 +607,11 @@ def expert_rows(tokens, k, n_experts, multiple=32):
 def expert_plan(experts, n_experts, multiple=32, rows=None):
     """dict(row_of [T,k], source [R], offsets [n_experts + 1]) of int32 tensors for experts [T,k] int32 (numbers outside
     [0, n_experts) are dropped); R is expert_rows(...) unless given."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.expert_plan(experts, n_experts, multiple, rows)
+        if done is not None:
+            return done
     import torch
     L = load()
     assert experts.dtype == torch.int32 and experts.dim() == 2 and experts.is_contiguous()
@@ -624,6 +651,11 @@ def _word_out(word, device):
 
 def expert_dispatch_bf16(x, plan, y=None, absmax_bits=None):
     """(y [R,C], max word): every token's row of x [T,C] in the rows that the plan gives it, zeros in the others."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.expert_dispatch_bf16(x, plan, y, absmax_bits)
+        if done is not None:
+            return done
     import torch
     L = load()
     row_of, source = _plan_of(plan)
@@ -641,6 +673,11 @@ def expert_dispatch_bf16(x, plan, y=None, absmax_bits=None):
 
 def expert_combine_bf16(y, plan, weights=None, out=None):
     """out[t] = sum_j weights[t,j] * y[row_of[t,j]] (weights [T,k] float32; None: 1, which is the gradient of the dispatch)."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.expert_combine_bf16(y, plan, weights, out)
+        if done is not None:
+            return done
     import torch
     L = load()
     row_of, source = _plan_of(plan)
@@ -658,6 +695,11 @@ def expert_combine_bf16(y, plan, weights=None, out=None):
 
 def expert_combine_bf16_backward(d_out, y, plan, weights, d_y=None, d_weights=None, absmax_bits=None):
     """(d_y [R,C], d_weights [T,k], max word of d_y) for the gradient d_out [T,C] of expert_combine_bf16(y, plan, weights)."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.expert_combine_bf16_backward(d_out, y, plan, weights, d_y, d_weights, absmax_bits)
+        if done is not None:
+            return done
     import torch
     L = load()
     row_of, source = _plan_of(plan)

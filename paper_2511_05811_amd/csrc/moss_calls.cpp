@@ -31,11 +31,20 @@ struct Library {
     decltype(&moss_internal_swiglu_bf16_backward) swiglu_bf16_backward;
     decltype(&moss_internal_add_rmsnorm_bf16) add_rmsnorm_bf16;
     decltype(&moss_internal_rmsnorm_bf16_backward) rmsnorm_bf16_backward;
+    decltype(&moss_quant_block128) quant_block128;
+    decltype(&moss_gemm_fp8_block128) gemm_fp8_block128;
+    decltype(&moss_gemm_fp8_mx_grouped) gemm_fp8_mx_grouped;
+    decltype(&moss_gemm_fp8_mx_grouped_dw) gemm_fp8_mx_grouped_dw;
+    decltype(&moss_expert_rows) expert_rows;
+    decltype(&moss_expert_plan) expert_plan;
+    decltype(&moss_internal_expert_dispatch_bf16) expert_dispatch_bf16;
+    decltype(&moss_expert_combine_bf16) expert_combine_bf16;
+    decltype(&moss_internal_expert_combine_bf16_backward) expert_combine_bf16_backward;
 };
 
 Library lib;
 PyObject *check = nullptr, *adamw_type = nullptr, *get_device = nullptr, *get_stream = nullptr;
-PyObject *k_q_row, *k_e_row, *k_q_col, *k_e_col, *k_s;
+PyObject *k_q_row, *k_e_row, *k_q_col, *k_e_col, *k_s, *k_s_row, *k_s_col, *k_row_of, *k_source, *k_offsets;
 
 bool plain_state() { return !at::impl::torch_function_mode_enabled() && !c10::impl::dispatch_mode_enabled(); }
 
@@ -467,6 +476,341 @@ PyObject *rmsnorm_bf16_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- blocks of 128 and experts.  Their Python code asks for tensors on the current GPU, so the current device is looked at first.
+
+// The device and its current stream; false with an exception set
+bool current_place(long &device, void *&stream)
+{
+    PyObject *d = PyObject_CallNoArgs(get_device);
+    if (!d) return false;
+    device = PyLong_AsLong(d);
+    PyObject *handle = PyObject_CallOneArg(get_stream, d);
+    Py_DECREF(d);
+    if (!handle) return false;
+    stream = PyLong_AsVoidPtr(handle);
+    Py_DECREF(handle);
+    return !PyErr_Occurred();
+}
+
+bool all_on(long device, std::initializer_list<const at::Tensor *> tensors)
+{
+    for (const at::Tensor *t : tensors)
+        if (t && t->device().index() != device) return false;
+    return true;
+}
+
+// a dense tensor of that type and shape
+bool dense(const at::Tensor *t, at::ScalarType type, at::IntArrayRef shape) { return t && t->scalar_type() == type && t->sizes() == shape && t->is_contiguous(); }
+
+// out[key] of a dict or None, if it is there a dense tensor of that type and shape, else a new one; false if it is another
+bool dense_out(PyObject *out, PyObject *key, Output &o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like)
+{
+    PyObject *given;
+    const at::Tensor *t;
+    if (!QuantOutputs::get(out, key, given, t)) return false;
+    if (t) {
+        if (!dense(t, type, shape)) return false;
+        o.take(given, t);
+    } else {
+        o.set(make(shape, type, like));
+    }
+    return true;
+}
+
+// rows of a [rows x cols] output: the caller's, or new ones
+bool matrix_out(PyObject *given, Output &o, int64_t rows, int64_t cols, at::ScalarType type, const at::Tensor &like)
+{
+    const at::Tensor *t;
+    if (!optional(given, t)) return false;
+    if (t) {
+        if (t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (cols > 1 && t->stride(1) != 1)) return false;
+        o.take(given, t);
+    } else {
+        o.set(make({rows, cols}, type, like));
+    }
+    return true;
+}
+
+int64_t row_stride(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
+
+// (x, flags, out)
+PyObject *quant_block128(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        unsigned flags;
+        const at::Tensor *x;
+        PLAIN_OR_NONE(n == 3 && plain_state() && (x = plain(a[0])) && rows_bf16(*x) && flags_of(a[1], flags) && (a[2] == Py_None || PyDict_CheckExact(a[2])));
+        const int64_t rows = x->size(0), cols = x->size(1);
+        Output qr, sr, qc, sc;
+        if (flags & MOSS_Q_ROW)
+            PLAIN_OR_NONE(dense_out(a[2], k_q_row, qr, at::kByte, {rows, cols}, *x) && dense_out(a[2], k_s_row, sr, at::kFloat, {rows, (cols + 127) / 128}, *x));
+        if (flags & MOSS_Q_COL)
+            PLAIN_OR_NONE(dense_out(a[2], k_q_col, qc, at::kByte, {cols, rows}, *x) && dense_out(a[2], k_s_col, sc, at::kFloat, {cols, (rows + 127) / 128}, *x));
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {x}));
+        void *px = ptr(x);
+        auto at = [](const Output &o) { return o.o ? o.t.data_ptr() : nullptr; };
+        uint8_t *pqr = (uint8_t *)at(qr), *pqc = (uint8_t *)at(qc);
+        float *psr = (float *)at(sr), *psc = (float *)at(sc);
+        const int64_t ld = row_stride(*x);
+        const int rc = without_gil([&] { return lib.quant_block128(px, rows, cols, ld, flags, pqr, psr, pqc, psc, stream); });
+        if (!checked(rc, "moss_quant_block128")) return nullptr;
+        PyObject *d = PyDict_New();
+        if (!d) return nullptr;
+        const std::pair<PyObject *, const Output *> items[4] = {{k_q_row, &qr}, {k_s_row, &sr}, {k_q_col, &qc}, {k_s_col, &sc}};
+        for (const auto &[key, value] : items)
+            if (PyDict_SetItem(d, key, value->o ? value->o : Py_None) < 0) {
+                Py_DECREF(d);
+                return nullptr;
+            }
+        return d;
+    });
+}
+
+// (a_q, a_s, b_q, b_s, out, accumulate); without `out` the result is BF16
+PyObject *gemm_fp8_block128(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *aq, *as, *bq, *bs;
+        PLAIN_OR_NONE(n == 6 && plain_state() && (aq = plain(a[0])) && (as = plain(a[1])) && (bq = plain(a[2])) && (bs = plain(a[3])) && PyBool_Check(a[5]));
+        PLAIN_OR_NONE(aq->dim() == 2 && bq->dim() == 2);
+        const int64_t M = aq->size(0), K = aq->size(1), N = bq->size(0), blocks = (K + 127) / 128, wide = (N + 127) / 128;
+        PLAIN_OR_NONE(dense(aq, at::kByte, {M, K}) && dense(bq, at::kByte, {N, K}) && dense(as, at::kFloat, {M, blocks}));
+        const bool of_weight = dense(bs, at::kFloat, {wide, blocks});
+        PLAIN_OR_NONE(of_weight || dense(bs, at::kFloat, {N, blocks}));
+        Output out;
+        PLAIN_OR_NONE(matrix_out(a[4], out, M, N, at::kBFloat16, *aq) && dtype_of(out.t) >= 0);
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {aq, as, bq, bs, &out.t}));
+        const uint8_t *pa = bytes(aq), *pb = bytes(bq);
+        const float *sa = (const float *)ptr(as), *sb = (const float *)ptr(bs);
+        void *po = ptr(&out.t);
+        const int dt = dtype_of(out.t), acc = a[5] == Py_True;
+        const int64_t ld = row_stride(out.t);
+        const int rc = without_gil([&] { return lib.gemm_fp8_block128(M, N, K, pa, sa, pb, sb, of_weight ? 128 : 1, po, dt, ld, acc, stream); });
+        return checked(rc, "moss_gemm_fp8_block128") ? out.release() : nullptr;
+    });
+}
+
+bool scalar_f32(const at::Tensor *t) { return t && t->scalar_type() == at::kFloat && t->numel() == 1; }
+bool offsets_ok(const at::Tensor *t) { return t && t->scalar_type() == at::kInt && t->dim() == 1 && t->size(0) >= 2 && t->is_contiguous(); }
+
+// (a_q, a_e, a_s, b_q, b_s, offsets, out, accumulate); without `out` the result is BF16
+PyObject *gemm_fp8_mx_grouped(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *aq, *ae, *as, *bq, *bs, *off;
+        PLAIN_OR_NONE(n == 8 && plain_state() && (aq = plain(a[0])) && optional(a[1], ae) && (as = plain(a[2])) && (bq = plain(a[3])) && (bs = plain(a[4])) &&
+                      (off = plain(a[5])) && PyBool_Check(a[7]));
+        PLAIN_OR_NONE(aq->dim() == 2 && bq->dim() == 3 && offsets_ok(off) && scalar_f32(as));
+        const int64_t R = aq->size(0), K = aq->size(1), G = bq->size(0), N = bq->size(1);
+        PLAIN_OR_NONE(dense(aq, at::kByte, {R, K}) && (!ae || dense(ae, at::kByte, {R, K / 32})) && bq->scalar_type() == at::kByte && bq->size(2) == K &&
+                      bq->stride(2) == 1 && off->size(0) == G + 1);
+        PLAIN_OR_NONE(bs->scalar_type() == at::kFloat && (bs->numel() == 1 || (bs->dim() == 1 && bs->size(0) == G)));
+        Output out;
+        PLAIN_OR_NONE(matrix_out(a[6], out, R, N, at::kBFloat16, *aq) && dtype_of(out.t) >= 0);
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {aq, ae, as, bq, bs, off, &out.t}));
+        const uint8_t *pa = bytes(aq), *pe = bytes(ae), *pb = bytes(bq);
+        const float *sa = (const float *)ptr(as), *sb = (const float *)ptr(bs);
+        const int32_t *po = (const int32_t *)ptr(off);
+        void *dst = ptr(&out.t);
+        const int dt = dtype_of(out.t), acc = a[7] == Py_True;
+        const int64_t ld = row_stride(out.t), ld_b = N > 1 ? bq->stride(1) : K, b_stride = G > 1 ? bq->stride(0) : 0, s_stride = bs->numel() > 1 ? bs->stride(0) : 0;
+        const int rc = without_gil([&] { return lib.gemm_fp8_mx_grouped(R, N, K, G, po, pa, pe, sa, pb, ld_b, b_stride, sb, s_stride, dst, dt, ld, acc, stream); });
+        return checked(rc, "moss_gemm_fp8_mx_grouped") ? out.release() : nullptr;
+    });
+}
+
+// (a_q, a_e, a_s, b_q, b_e, b_s, offsets, out, accumulate)
+PyObject *gemm_fp8_mx_grouped_dw(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *aq, *ae, *as, *bq, *be, *bs, *off, *given;
+        PLAIN_OR_NONE(n == 9 && plain_state() && (aq = plain(a[0])) && (ae = plain(a[1])) && (as = plain(a[2])) && (bq = plain(a[3])) && (be = plain(a[4])) &&
+                      (bs = plain(a[5])) && (off = plain(a[6])) && optional(a[7], given) && PyBool_Check(a[8]));
+        PLAIN_OR_NONE(aq->dim() == 2 && bq->dim() == 2 && offsets_ok(off) && scalar_f32(as) && scalar_f32(bs));
+        const int64_t M = aq->size(0), R = aq->size(1), N = bq->size(0), G = off->size(0) - 1;
+        PLAIN_OR_NONE(dense(aq, at::kByte, {M, R}) && dense(bq, at::kByte, {N, R}) && dense(ae, at::kByte, {M, R / 32}) && dense(be, at::kByte, {N, R / 32}));
+        Output out;
+        if (given) {
+            PLAIN_OR_NONE(dtype_of(*given) >= 0 && dense(given, given->scalar_type(), {G, M, N}));
+            out.take(a[7], given);
+        } else {
+            out.set(make({G, M, N}, at::kFloat, *aq));
+        }
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {aq, ae, as, bq, be, bs, off, &out.t}));
+        const uint8_t *pa = bytes(aq), *pae = bytes(ae), *pb = bytes(bq), *pbe = bytes(be);
+        const float *sa = (const float *)ptr(as), *sb = (const float *)ptr(bs);
+        const int32_t *po = (const int32_t *)ptr(off);
+        void *dst = ptr(&out.t);
+        const int dt = dtype_of(out.t), acc = a[8] == Py_True;
+        const int rc = without_gil([&] { return lib.gemm_fp8_mx_grouped_dw(R, M, N, G, po, pa, pae, sa, pb, pbe, sb, dst, dt, acc, stream); });
+        return checked(rc, "moss_gemm_fp8_mx_grouped_dw") ? out.release() : nullptr;
+    });
+}
+
+bool whole(PyObject *o, int64_t &v)
+{
+    if (!PyLong_CheckExact(o)) return false;
+    int overflow;
+    v = PyLong_AsLongLongAndOverflow(o, &overflow);
+    return !overflow;
+}
+
+// (experts, n_experts, multiple, rows)
+PyObject *expert_plan(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *e;
+        int64_t E, multiple, rows;
+        PLAIN_OR_NONE(n == 4 && plain_state() && (e = plain(a[0])) && e->scalar_type() == at::kInt && e->dim() == 2 && e->is_contiguous() && whole(a[1], E) &&
+                      whole(a[2], multiple) && (a[3] == Py_None || whole(a[3], rows)));
+        const int64_t T = e->size(0), k = e->size(1);
+        if (a[3] == Py_None) rows = lib.expert_rows(T, k, E, multiple);
+        PLAIN_OR_NONE(rows > 0 && rows <= 0x7FFFFFFF && E > 0 && E <= 0x7FFFFFF);
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {e}));
+        Output row_of, source, offsets;
+        row_of.set(make({T, k}, at::kInt, *e));
+        source.set(make({rows}, at::kInt, *e));
+        offsets.set(make({E + 1}, at::kInt, *e));
+        const int32_t *pe = (const int32_t *)ptr(e);
+        int32_t *pr = (int32_t *)ptr(&row_of.t), *ps = (int32_t *)ptr(&source.t), *po = (int32_t *)ptr(&offsets.t);
+        const int rc = without_gil([&] { return lib.expert_plan(pe, T, k, E, multiple, rows, pr, ps, po, stream); });
+        if (!checked(rc, "moss_expert_plan")) return nullptr;
+        PyObject *d = PyDict_New();
+        if (!d) return nullptr;
+        if (PyDict_SetItem(d, k_row_of, row_of.o) < 0 || PyDict_SetItem(d, k_source, source.o) < 0 || PyDict_SetItem(d, k_offsets, offsets.o) < 0) {
+            Py_DECREF(d);
+            return nullptr;
+        }
+        return d;
+    });
+}
+
+struct Plan {
+    const at::Tensor *row_of = nullptr, *source = nullptr;
+    bool of(PyObject *o)
+    {
+        if (!PyDict_CheckExact(o)) return false;
+        PyObject *r = PyDict_GetItem(o, k_row_of), *s = PyDict_GetItem(o, k_source);
+        return r && s && (row_of = plain(r)) && (source = plain(s)) && row_of->scalar_type() == at::kInt && source->scalar_type() == at::kInt &&
+               row_of->dim() == 2 && source->dim() == 1 && row_of->is_contiguous() && source->is_contiguous();
+    }
+    int64_t tokens() const { return row_of->size(0); }
+    int64_t k() const { return row_of->size(1); }
+    int64_t rows() const { return source->size(0); }
+    const int32_t *row_of_ptr() const { return (const int32_t *)row_of->data_ptr(); }
+    const int32_t *source_ptr() const { return (const int32_t *)source->data_ptr(); }
+};
+
+bool bf16_of(const at::Tensor *t, int64_t rows) { return t && rows_bf16(*t) && t->size(0) == rows; }
+bool bf16_rows_out(const Output &o) { return o.t.scalar_type() == at::kBFloat16 && o.t.stride(1) == 1; }
+
+// (x, plan, y, absmax_bits)
+PyObject *expert_dispatch_bf16(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *x;
+        Plan plan;
+        PLAIN_OR_NONE(n == 4 && plain_state() && (x = plain(a[0])) && plan.of(a[1]) && bf16_of(x, plan.tokens()));
+        const int64_t T = plan.tokens(), k = plan.k(), R = plan.rows(), C = x->size(1);
+        Output y, top;
+        PLAIN_OR_NONE(matrix_out(a[2], y, R, C, at::kBFloat16, *x) && bf16_rows_out(y) && word(a[3], top, *x) && top.t.scalar_type() == at::kInt && top.t.numel() == 1);
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {x, plan.row_of, plan.source, &y.t, &top.t}));
+        const int64_t ld_x = row_stride(*x), ld_y = row_stride(y.t);
+        void *px = ptr(x), *py = ptr(&y.t);
+        const int32_t *pr = plan.row_of_ptr(), *ps = plan.source_ptr();
+        uint32_t *w = word_ptr(top);
+        const at::Tensor ws = producer_workspace(*x);
+        void *pw = ws.data_ptr();
+        const int rc = without_gil([&] { return lib.expert_dispatch_bf16(px, pr, ps, T, k, R, C, ld_x, ld_y, py, w, pw, kProducerWorkspaceBytes, stream); });
+        return checked(rc, "moss_expert_dispatch_bf16") ? PyTuple_Pack(2, y.o, top.o) : nullptr;
+    });
+}
+
+// (y, plan, weights, out)
+PyObject *expert_combine_bf16(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *y, *weights;
+        Plan plan;
+        PLAIN_OR_NONE(n == 4 && plain_state() && (y = plain(a[0])) && plan.of(a[1]) && optional(a[2], weights) && bf16_of(y, plan.rows()));
+        const int64_t T = plan.tokens(), k = plan.k(), R = plan.rows(), C = y->size(1);
+        PLAIN_OR_NONE(!weights || dense(weights, at::kFloat, {T, k}));
+        Output out;
+        PLAIN_OR_NONE(matrix_out(a[3], out, T, C, at::kBFloat16, *y) && bf16_rows_out(out));
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {y, plan.row_of, weights, &out.t}));
+        const int64_t ld_y = row_stride(*y), ld_out = row_stride(out.t);
+        void *py = ptr(y), *po = ptr(&out.t);
+        const int32_t *pr = plan.row_of_ptr();
+        const float *pw = (const float *)ptr(weights);
+        const int rc = without_gil([&] { return lib.expert_combine_bf16(py, pr, pw, T, k, R, C, ld_y, ld_out, po, stream); });
+        return checked(rc, "moss_expert_combine_bf16") ? out.release() : nullptr;
+    });
+}
+
+// (d_out, y, plan, weights, d_y, d_weights, absmax_bits)
+PyObject *expert_combine_bf16_backward(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *d_out, *y, *weights, *given, *given_w;
+        Plan plan;
+        PLAIN_OR_NONE(n == 7 && plain_state() && (d_out = plain(a[0])) && (y = plain(a[1])) && plan.of(a[2]) && (weights = plain(a[3])) && optional(a[4], given) &&
+                      optional(a[5], given_w));
+        const int64_t T = plan.tokens(), k = plan.k(), R = plan.rows();
+        PLAIN_OR_NONE(bf16_of(d_out, T) && bf16_of(y, R) && y->size(1) == d_out->size(1) && dense(weights, at::kFloat, {T, k}));
+        const int64_t C = d_out->size(1), ld_y = row_stride(*y), ld_out = row_stride(*d_out);
+        Output d_y, d_w, top;
+        if (given) {
+            PLAIN_OR_NONE(bf16_of(given, R) && given->size(1) == C && row_stride(*given) == ld_y);
+            d_y.take(a[4], given);
+        } else {
+            d_y.set(at::empty_strided({R, C}, {ld_y, 1}, at::TensorOptions().dtype(at::kBFloat16).device(y->device())));
+        }
+        if (given_w) {
+            PLAIN_OR_NONE(dense(given_w, at::kFloat, {T, k}));
+            d_w.take(a[5], given_w);
+        } else {
+            d_w.set(make({T, k}, at::kFloat, *y));
+        }
+        PLAIN_OR_NONE(word(a[6], top, *y) && top.t.scalar_type() == at::kInt && top.t.numel() == 1);
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {d_out, y, plan.row_of, plan.source, weights, &d_y.t, &d_w.t, &top.t}));
+        void *pd = ptr(d_out), *py = ptr(y), *po = ptr(&d_y.t);
+        const int32_t *pr = plan.row_of_ptr(), *ps = plan.source_ptr();
+        const float *pw = (const float *)ptr(weights);
+        float *pdw = (float *)ptr(&d_w.t);
+        uint32_t *w = word_ptr(top);
+        const at::Tensor ws = producer_workspace(*y);
+        void *pws = ws.data_ptr();
+        const int rc = without_gil([&] {
+            return lib.expert_combine_bf16_backward(pd, py, pr, ps, pw, T, k, R, C, ld_out, ld_y, po, pdw, w, pws, kProducerWorkspaceBytes, stream);
+        });
+        return checked(rc, "moss_expert_combine_bf16_backward") ? PyTuple_Pack(3, d_y.o, d_w.o, top.o) : nullptr;
+    });
+}
+
 // (addresses of the library's functions in the order of Library, _check, AdamWArgs, torch's current device and raw stream)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -493,7 +837,9 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 #define CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(bind), CALL(quant_act_2level), CALL(quant_act_2level_given_max), CALL(gemm_fp8_mx), CALL(weight_autoscale_cast),
-                         CALL(swiglu_bf16), CALL(swiglu_bf16_backward), CALL(add_rmsnorm_bf16), CALL(rmsnorm_bf16_backward),
+                         CALL(swiglu_bf16), CALL(swiglu_bf16_backward), CALL(add_rmsnorm_bf16), CALL(rmsnorm_bf16_backward), CALL(quant_block128), CALL(gemm_fp8_block128),
+                         CALL(gemm_fp8_mx_grouped), CALL(gemm_fp8_mx_grouped_dw), CALL(expert_plan), CALL(expert_dispatch_bf16),
+                         CALL(expert_combine_bf16), CALL(expert_combine_bf16_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_moss_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -506,7 +852,12 @@ PyMODINIT_FUNC PyInit__moss_calls()
     k_q_col = PyUnicode_InternFromString("q_col");
     k_e_col = PyUnicode_InternFromString("e_col");
     k_s = PyUnicode_InternFromString("s");
-    if (!k_q_row || !k_e_row || !k_q_col || !k_e_col || !k_s) return nullptr;
+    k_s_row = PyUnicode_InternFromString("s_row");
+    k_s_col = PyUnicode_InternFromString("s_col");
+    k_row_of = PyUnicode_InternFromString("row_of");
+    k_source = PyUnicode_InternFromString("source");
+    k_offsets = PyUnicode_InternFromString("offsets");
+    if (!k_q_row || !k_e_row || !k_q_col || !k_e_col || !k_s || !k_s_row || !k_s_col || !k_row_of || !k_source || !k_offsets) return nullptr;
     PyObject *m = PyModule_Create(&module);
     // what this was compiled for: binding.py compares it with the torch and the library that it has before it binds anything
     if (m && (PyModule_AddStringConstant(m, "torch_version", MOSS_TORCH_VERSION) < 0 ||
