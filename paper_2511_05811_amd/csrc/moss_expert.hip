@@ -4,7 +4,7 @@
 //
 // Bound: HBM.  Everything goes by tokens: a token's row is read once and stays in registers while its k rows are written (dispatch) or
 // multiplied (gradient of combine); rows of zeros between the experts' rows are items of their own behind the tokens.  16 bytes
-// per thread, 32 to 256 threads per token by the width.  Sums and products in FP32, one rounding to BF16 at the end.  The tensors
+// per thread, half a wave or a wave per token.  Sums and products in FP32, one rounding to BF16 at the end.  The tensors
 // that a quantizer reads leave their maximum behind, as the other BF16 producers do.
 #include "moss_internal.h"
 #include "moss_producer.h"
@@ -15,6 +15,7 @@ namespace {
 constexpr int kExThreads = 256;
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
+constexpr int kPlanMaxWgs = 64;
 constexpr int kMaxExperts = 1024;
 
 typedef unsigned short ex_u16x2 __attribute__((ext_vector_type(2)));
@@ -39,47 +40,56 @@ __device__ __forceinline__ uint32_t ex_top(uint32_t m, uint4 v)
     return ex_pk_max(m, v.w & 0x7FFF7FFFu);
 }
 
-// The plan, by one workgroup.  Every wave has a contiguous part of the assignments and counts it per expert; a scan over
-// experts and waves gives each (wave, expert) its first row; then every wave walks its part again.  Of 64 assignments at a time, those of the
-// same expert are found bit by bit of its number with ballots, so that each knows how many are ahead of it and the order is kept.
+// The plan.  A workgroup places a contiguous part of the assignments, and counts all of them per expert for itself: those ahead of its
+// part, its own wave by wave, and those behind.  So the workgroups need nothing of each other.  A scan over experts and waves gives
+// each (wave, expert) its first row; then every wave walks its part again.  Of 64 assignments at a time, those of the same expert are
+// found bit by bit of its number with ballots, so that each knows how many are ahead of it and the order is kept.
+// (One workgroup for all: 16384 assignments 16 us.)
 __global__ __launch_bounds__(kPlanThreads) void k_expert_plan(const int32_t *__restrict__ experts, int64_t n, int E, int bits, int multiple, int64_t rows,
-                                                              int32_t *__restrict__ row_of, int32_t *__restrict__ source, int32_t *__restrict__ offsets)
+                                                              int64_t part, int32_t *__restrict__ row_of, int32_t *__restrict__ source,
+                                                              int32_t *__restrict__ offsets)
 {
     extern __shared__ int32_t first[];                // [waves][E]: counts, then first rows
+    int32_t *ahead_of_us = first + kPlanWaves * E, *behind_us = ahead_of_us + E;
     __shared__ int32_t sums[kPlanWaves];
+    constexpr int kAhead = 8;                         // (a step is a trip to memory: eight are under way together)
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t steps = (n + kWave - 1) / kWave, per = (steps + kPlanWaves - 1) / kPlanWaves;
-    const int64_t from = wave * per * kWave, to = from + per * kWave < n ? from + per * kWave : n;
-    for (int i = tid; i < kPlanWaves * E; i += kPlanThreads) first[i] = 0;
+    const int64_t begin = (int64_t)blockIdx.x * part, end = begin + part < n ? begin + part : n;
+    const int64_t per = ((end - begin + kWave - 1) / kWave + kPlanWaves - 1) / kPlanWaves * kWave;
+    const int64_t from = begin + wave * per < end ? begin + wave * per : end, to = from + per < end ? from + per : end;
+    for (int i = tid; i < (kPlanWaves + 2) * E; i += kPlanThreads) first[i] = 0;
     __syncthreads();
-    auto expert_at = [&](int64_t a) {
-        const int e = a < to ? experts[a] : -1;
-        return e >= 0 && e < E ? e : -1;
+    // the experts of assignments a0, a0 + stride, ..., -1 for none
+    auto load_experts = [&](int (&e)[kAhead], int64_t a0, int stride, int64_t stop) {
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) e[u] = a0 + u * stride < stop ? experts[a0 + u * stride] : -1;
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) e[u] = e[u] < E && e[u] >= 0 ? e[u] : -1;
     };
-    // lanes of the wave with the same expert (those without one are with each other)
-    auto same = [&](int e) {
-        uint64_t m = __ballot(e >= 0);
-        if (e < 0) m = ~m;
-        for (int b = 0; b < bits; b++) {
-            const uint64_t set = __ballot((e >> b) & 1);
-            m &= (e >> b) & 1 ? set : ~set;
+    auto count = [&](int32_t *into, int64_t start, int64_t stop, int stride, int64_t batch) {
+        for (int64_t a = start; a < stop; a += batch) {
+            int e[kAhead];
+            load_experts(e, a, stride, stop);
+#pragma unroll
+            for (int u = 0; u < kAhead; u++)
+                if (e[u] >= 0) atomicAdd(&into[e[u]], 1);
         }
-        return m;
     };
-    for (int64_t a0 = from; a0 < to; a0 += kWave) {
-        const int e = expert_at(a0 + lane);
-        if (e >= 0) atomicAdd(&first[wave * E + e], 1);           // (the wave's own counters)
-    }
+    count(ahead_of_us, tid, begin, kPlanThreads, (int64_t)kPlanThreads * kAhead);
+    count(behind_us, end + tid, n, kPlanThreads, (int64_t)kPlanThreads * kAhead);
+    count(first + wave * E, from + lane, to, kWave, (int64_t)kWave * kAhead);
     __syncthreads();
     // thread e: rows of expert e, filled up; scan over the threads
-    int count = 0, filled = 0;
+    int total = 0, filled = 0;
     if (tid < E) {
+        total = ahead_of_us[tid];
         for (int w = 0; w < kPlanWaves; w++) {
             const int c = first[w * E + tid];
-            first[w * E + tid] = count;
-            count += c;
+            first[w * E + tid] = total;
+            total += c;
         }
-        filled = (count + multiple - 1) / multiple * multiple;
+        total += behind_us[tid];
+        filled = (total + multiple - 1) / multiple * multiple;
     }
     int upto = filled;
 #pragma unroll
@@ -93,28 +103,43 @@ __global__ __launch_bounds__(kPlanThreads) void k_expert_plan(const int32_t *__r
     if (tid < E) {
         const int start = upto - filled;
         for (int w = 0; w < kPlanWaves; w++) first[w * E + tid] += start;
-        offsets[tid] = start;
-        if (tid == E - 1) offsets[E] = (int32_t)rows;
-        for (int r = start + count; r < upto; r++) source[r] = -1;
+        if (blockIdx.x == 0) {
+            offsets[tid] = start;
+            if (tid == E - 1) offsets[E] = (int32_t)rows;
+        }
+        if (tid % gridDim.x == blockIdx.x)
+            for (int r = start + total; r < upto; r++) source[r] = -1;
     }
     __syncthreads();
     int all = 0;
     for (int w = 0; w < kPlanWaves; w++) all += sums[w];
-    for (int64_t r = all + tid; r < rows; r += kPlanThreads) source[r] = -1;
-    for (int64_t a0 = from; a0 < to; a0 += kWave) {
-        const int64_t a = a0 + lane;
-        const int e = expert_at(a);
-        const uint64_t mine = same(e);
-        const int ahead = __popcll(mine & ((1ull << lane) - 1));
-        int row = -1;
-        if (e >= 0) {
-            row = first[wave * E + e] + ahead;
-            source[row] = (int32_t)a;
+    for (int64_t r = all + (int64_t)blockIdx.x * kPlanThreads + tid; r < rows; r += (int64_t)gridDim.x * kPlanThreads) source[r] = -1;
+    for (int64_t a0 = from; a0 < to; a0 += kWave * kAhead) {
+        int es[kAhead];
+        load_experts(es, a0 + lane, kWave, to);
+#pragma unroll
+        for (int u = 0; u < kAhead; u++) {
+            if (a0 + u * kWave >= to) break;
+            const int64_t a = a0 + u * kWave + lane;
+            const int e = es[u];
+            // lanes of the wave with the same expert (those without one are with each other)
+            uint64_t mine = __ballot(e >= 0);
+            if (e < 0) mine = ~mine;
+            for (int b = 0; b < bits; b++) {
+                const uint64_t set = __ballot((e >> b) & 1);
+                mine &= (e >> b) & 1 ? set : ~set;
+            }
+            const int ahead = __popcll(mine & ((1ull << lane) - 1));
+            int row = -1;
+            if (e >= 0) {
+                row = first[wave * E + e] + ahead;
+                source[row] = (int32_t)a;
+            }
+            if (a < to) row_of[a] = row;
+            __builtin_amdgcn_wave_barrier();                      // (all lanes have read their counters)
+            if (e >= 0 && ahead == 0) first[wave * E + e] += __popcll(mine);
+            __builtin_amdgcn_wave_barrier();
         }
-        if (a < to) row_of[a] = row;
-        __builtin_amdgcn_wave_barrier();                          // (all lanes have read their counters)
-        if (e >= 0 && ahead == 0) first[wave * E + e] += __popcll(mine);
-        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -155,108 +180,140 @@ struct ExArgs {
     int flags;
 };
 
-__device__ __forceinline__ bool row_ok(int r, int64_t rows) { return r >= 0 && r < rows; }
+__device__ __forceinline__ int row_or_none(int r, int64_t rows) { return r >= 0 && r < rows ? r : -1; }
+
+// A token is worked on by LANES threads of one wave, which have kDeep chunks of each row under way; of its choices K at a time.
+constexpr int kDeep = 4;
+
+template <int K>
+__device__ __forceinline__ void load_rows(int (&r)[K], const ExArgs &p, int64_t token, int j0)
+{
+#pragma unroll
+    for (int j = 0; j < K; j++) r[j] = j0 + j < p.k ? row_or_none(p.row_of[token * p.k + j0 + j], p.rows) : -1;
+}
 
 // Tokens, then rows without one (zeros).  GRAD: gradient of combine, else dispatch.
-template <bool GRAD, int LANES>
+template <bool GRAD, int LANES, int K>
 __global__ __launch_bounds__(kExThreads) void k_expert_scatter(const ExArgs p, MaxSlots slots)
 {
     constexpr int kItems = kExThreads / LANES;
-    __shared__ float part[GRAD && LANES > kWave ? kExThreads / kWave : 1];
-    const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
+    const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES, stream = p.flags & kProducerStream;
     uint32_t m = 0;
-    for (int64_t i0 = (int64_t)blockIdx.x * kItems; i0 < p.tokens + p.rows; i0 += (int64_t)gridDim.x * kItems) {
-        const int64_t i = i0 + slot;
+    for (int64_t i = (int64_t)blockIdx.x * kItems + slot; i < p.tokens + p.rows; i += (int64_t)gridDim.x * kItems) {
         if (i >= p.tokens) {
             const int64_t r = i - p.tokens;
-            if (r < p.rows) {
-                const int a = p.source[r];
-                if (!(a >= 0 && a < p.tokens * p.k))
-                    for (int c = sub; c < p.chunks; c += LANES) st_producer16(p.out + r * p.ld_out + (int64_t)c * 8, make_uint4(0, 0, 0, 0), p.flags & kProducerStream);
-            }
-        }
-        const bool token = i < p.tokens;
-        if (!GRAD) {
-            if (!token) continue;
-            for (int c = sub; c < p.chunks; c += LANES) {
-                const uint4 v = ld_stream16(p.x + i * p.ld_x + (int64_t)c * 8);
-                bool used = false;
-                for (int j = 0; j < p.k; j++) {
-                    const int r = p.row_of[i * p.k + j];
-                    if (!row_ok(r, p.rows)) continue;
-                    used = true;
-                    st_producer16(p.out + (int64_t)r * p.ld_out + (int64_t)c * 8, v, p.flags & kProducerStream);
-                }
-                if (used) m = ex_top(m, v);
-            }
+            const int a = p.source[r];
+            if (!(a >= 0 && a < p.tokens * p.k))
+                for (int c = sub; c < p.chunks; c += LANES) st_producer16(p.out + r * p.ld_out + (int64_t)c * 8, make_uint4(0, 0, 0, 0), stream);
             continue;
         }
-        for (int j = 0; j < p.k; j++) {
-            float dot = 0.0f;
-            if (token) {
-                const int r = p.row_of[i * p.k + j];
-                if (row_ok(r, p.rows)) {
-                    const float w = p.weights[i * p.k + j];
-                    for (int c = sub; c < p.chunks; c += LANES) {
-                        const uint4 g = *reinterpret_cast<const uint4 *>(p.x + i * p.ld_x + (int64_t)c * 8);
-                        const uint4 v = ld_stream16(p.y + (int64_t)r * p.ld_y + (int64_t)c * 8);
-                        const uint32_t a[4] = {g.x, g.y, g.z, g.w}, b[4] = {v.x, v.y, v.z, v.w};
-                        uint32_t o[4];
+        const uint16_t *x = p.x + i * p.ld_x;
+        for (int j0 = 0; j0 < p.k; j0 += K) {
+            int r[K];
+            load_rows(r, p, i, j0);
+            float w[K], dot[K];
 #pragma unroll
-                        for (int q = 0; q < 4; q++) {
-                            dot += ex_lo(a[q]) * ex_lo(b[q]) + ex_hi(a[q]) * ex_hi(b[q]);
-                            o[q] = ex_pack(w * ex_lo(a[q]), w * ex_hi(a[q]));
+            for (int j = 0; j < K; j++) {
+                w[j] = GRAD && r[j] >= 0 ? p.weights[i * p.k + j0 + j] : 0.0f;
+                dot[j] = 0.0f;
+            }
+            for (int c0 = sub; c0 < p.chunks; c0 += LANES * kDeep) {
+                uint4 g[kDeep], v[kDeep][GRAD ? K : 1];
+#pragma unroll
+                for (int u = 0; u < kDeep; u++) {
+                    const int c = c0 + u * LANES;
+                    if (c >= p.chunks) continue;
+                    g[u] = *reinterpret_cast<const uint4 *>(x + (int64_t)c * 8);
+                    if (GRAD)
+#pragma unroll
+                        for (int j = 0; j < K; j++)
+                            if (r[j] >= 0) v[u][GRAD ? j : 0] = ld_stream16(p.y + (int64_t)r[j] * p.ld_y + (int64_t)c * 8);
+                }
+#pragma unroll
+                for (int u = 0; u < kDeep; u++) {
+                    const int c = c0 + u * LANES;
+                    if (c >= p.chunks) continue;
+#pragma unroll
+                    for (int j = 0; j < K; j++) {
+                        if (r[j] < 0) continue;
+                        uint4 d = g[u];
+                        if (GRAD) {
+                            const uint4 t = v[u][GRAD ? j : 0];
+                            const uint32_t a[4] = {g[u].x, g[u].y, g[u].z, g[u].w}, b[4] = {t.x, t.y, t.z, t.w};
+                            uint32_t o[4];
+#pragma unroll
+                            for (int q = 0; q < 4; q++) {
+                                dot[j] += ex_lo(a[q]) * ex_lo(b[q]) + ex_hi(a[q]) * ex_hi(b[q]);
+                                o[q] = ex_pack(w[j] * ex_lo(a[q]), w[j] * ex_hi(a[q]));
+                            }
+                            d = make_uint4(o[0], o[1], o[2], o[3]);
                         }
-                        const uint4 d = make_uint4(o[0], o[1], o[2], o[3]);
                         m = ex_top(m, d);
-                        st_producer16(p.out + (int64_t)r * p.ld_out + (int64_t)c * 8, d, p.flags & kProducerStream);
+                        st_producer16(p.out + (int64_t)r[j] * p.ld_out + (int64_t)c * 8, d, stream);
                     }
                 }
             }
+            if (GRAD) {
 #pragma unroll
-            for (int d = (LANES < kWave ? LANES : kWave) / 2; d > 0; d >>= 1) dot += __shfl_xor(dot, d, 64);
-            if (LANES > kWave) {
-                __syncthreads();
-                if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = dot;
-                __syncthreads();
-                dot = 0.0f;
+                for (int j = 0; j < K; j++) {
 #pragma unroll
-                for (int w = 0; w < LANES / kWave; w++) dot += part[slot * (LANES / kWave) + w];
+                    for (int d = LANES / 2; d > 0; d >>= 1) dot[j] += __shfl_xor(dot[j], d, 64);
+                    if (sub == 0 && j0 + j < p.k) p.d_weights[i * p.k + j0 + j] = dot[j];
+                }
             }
-            if (token && sub == 0) p.d_weights[i * p.k + j] = dot;
         }
     }
     finish_max(m, p.top, p.flags & kProducerLook, slots);
 }
 
 // out[t] = sum over j of weights[t, j] * x[row_of[t, j]], in the order of j; WEIGHTS false: the plain sum (gradient of dispatch)
-template <bool WEIGHTS, int LANES>
+template <bool WEIGHTS, int LANES, int K>
 __global__ __launch_bounds__(kExThreads) void k_expert_combine(const ExArgs p)
 {
     constexpr int kItems = kExThreads / LANES;
     const int sub = threadIdx.x % LANES, slot = threadIdx.x / LANES;
     for (int64_t i = (int64_t)blockIdx.x * kItems + slot; i < p.tokens; i += (int64_t)gridDim.x * kItems) {
-        for (int c = sub; c < p.chunks; c += LANES) {
-            float s[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            for (int j = 0; j < p.k; j++) {
-                const int r = p.row_of[i * p.k + j];
-                if (!row_ok(r, p.rows)) continue;
-                const uint4 v = ld_stream16(p.x + (int64_t)r * p.ld_x + (int64_t)c * 8);
-                const uint32_t a[4] = {v.x, v.y, v.z, v.w};
-                const float w = WEIGHTS ? p.weights[i * p.k + j] : 1.0f;
+        for (int c0 = sub; c0 < p.chunks; c0 += LANES * kDeep) {
+            float s[kDeep][8];
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    s[2 * q] += w * ex_lo(a[q]);
-                    s[2 * q + 1] += w * ex_hi(a[q]);
+            for (int u = 0; u < kDeep; u++)
+#pragma unroll
+                for (int q = 0; q < 8; q++) s[u][q] = 0.0f;
+            for (int j0 = 0; j0 < p.k; j0 += K) {
+                int r[K];
+                load_rows(r, p, i, j0);
+                uint4 v[kDeep][K];
+#pragma unroll
+                for (int j = 0; j < K; j++)
+#pragma unroll
+                    for (int u = 0; u < kDeep; u++)
+                        if (r[j] >= 0 && c0 + u * LANES < p.chunks) v[u][j] = ld_stream16(p.x + (int64_t)r[j] * p.ld_x + (int64_t)(c0 + u * LANES) * 8);
+#pragma unroll
+                for (int j = 0; j < K; j++) {
+                    if (r[j] < 0) continue;
+                    const float w = WEIGHTS ? p.weights[i * p.k + j0 + j] : 1.0f;
+#pragma unroll
+                    for (int u = 0; u < kDeep; u++) {
+                        if (c0 + u * LANES >= p.chunks) continue;
+                        const uint32_t a[4] = {v[u][j].x, v[u][j].y, v[u][j].z, v[u][j].w};
+#pragma unroll
+                        for (int q = 0; q < 4; q++) {
+                            s[u][2 * q] += w * ex_lo(a[q]);
+                            s[u][2 * q + 1] += w * ex_hi(a[q]);
+                        }
+                    }
                 }
             }
-            const uint4 o = make_uint4(ex_pack(s[0], s[1]), ex_pack(s[2], s[3]), ex_pack(s[4], s[5]), ex_pack(s[6], s[7]));
-            st_producer16(p.out + i * p.ld_out + (int64_t)c * 8, o, p.flags & kProducerStream);
+#pragma unroll
+            for (int u = 0; u < kDeep; u++) {
+                const int c = c0 + u * LANES;
+                if (c >= p.chunks) continue;
+                const uint4 o = make_uint4(ex_pack(s[u][0], s[u][1]), ex_pack(s[u][2], s[u][3]), ex_pack(s[u][4], s[u][5]), ex_pack(s[u][6], s[u][7]));
+                st_producer16(p.out + i * p.ld_out + (int64_t)c * 8, o, p.flags & kProducerStream);
+            }
         }
     }
 }
-
-int lanes_for(int chunks) { return chunks <= 32 ? 32 : chunks <= 64 ? 64 : chunks <= 128 ? 128 : 256; }
 
 int64_t device_cus()
 {
@@ -266,7 +323,7 @@ int64_t device_cus()
 
 int items_grid(int64_t items, int lanes)
 {
-    const int64_t wgs = (items + kExThreads / lanes - 1) / (kExThreads / lanes), most = device_cus() * 4;
+    const int64_t wgs = (items + kExThreads / lanes - 1) / (kExThreads / lanes), most = device_cus() * 8;
     return (int)(wgs < most ? wgs : most);
 }
 
@@ -278,27 +335,22 @@ int check_rows(int64_t tokens, int64_t k, int64_t rows, int64_t cols, int64_t ld
     return ld_tokens % 8 || ld_rows % 8 ? MOSS_ERR_ALIGN : MOSS_OK;
 }
 
-#define MOSS_EX_LANES(kernel_of, ...)                                                    \
-    switch (lanes) {                                                                      \
-        case 32: hipLaunchKernelGGL((kernel_of(32)), __VA_ARGS__); break;                  \
-        case 64: hipLaunchKernelGGL((kernel_of(64)), __VA_ARGS__); break;                  \
-        case 128: hipLaunchKernelGGL((kernel_of(128)), __VA_ARGS__); break;                \
-        default: hipLaunchKernelGGL((kernel_of(256)), __VA_ARGS__); break;                 \
-    }
+// the kernel of a width and a number of choices
+#define MOSS_EX_PICK(kernel, flag)                                                                                             \
+    (p.k == 1 ? (lanes == 32 ? kernel<flag, 32, 1> : kernel<flag, 64, 1>)                                                       \
+              : p.k == 2 ? (lanes == 32 ? kernel<flag, 32, 2> : kernel<flag, 64, 2>) : (lanes == 32 ? kernel<flag, 32, 4> : kernel<flag, 64, 4>))
 
 template <bool GRAD>
 int launch_scatter(ExArgs p, void *workspace, size_t workspace_bytes, hipStream_t st)
 {
-    const int lanes = lanes_for(p.chunks), grid = items_grid(p.tokens + p.rows, lanes);
+    const int lanes = p.chunks <= 32 ? 32 : 64, grid = items_grid(p.tokens + p.rows, lanes);
     p.flags = producer_flags(p.rows, (int64_t)p.chunks * 8, true);
     const MaxSlots slots = max_slots(workspace, workspace_bytes, grid, 1, st);
     if (!slots.call) {
         hipLaunchKernelGGL(k_expert_clear, dim3(1), dim3(64), 0, st, p.top);
         MOSS_LAUNCH_CHECK();
     }
-#define MOSS_EX_KERNEL(L) k_expert_scatter<GRAD, L>
-    MOSS_EX_LANES(MOSS_EX_KERNEL, dim3(grid), dim3(kExThreads), 0, st, p, slots)
-#undef MOSS_EX_KERNEL
+    hipLaunchKernelGGL(MOSS_EX_PICK(k_expert_scatter, GRAD), dim3(grid), dim3(kExThreads), 0, st, p, slots);
     MOSS_LAUNCH_CHECK();
     return MOSS_OK;
 }
@@ -306,11 +358,9 @@ int launch_scatter(ExArgs p, void *workspace, size_t workspace_bytes, hipStream_
 template <bool WEIGHTS>
 int launch_combine(ExArgs p, hipStream_t st)
 {
-    const int lanes = lanes_for(p.chunks), grid = items_grid(p.tokens, lanes);
+    const int lanes = p.chunks <= 32 ? 32 : 64, grid = items_grid(p.tokens, lanes);
     p.flags = producer_flags(p.tokens, (int64_t)p.chunks * 8, false);
-#define MOSS_EX_KERNEL(L) k_expert_combine<WEIGHTS, L>
-    MOSS_EX_LANES(MOSS_EX_KERNEL, dim3(grid), dim3(kExThreads), 0, st, p)
-#undef MOSS_EX_KERNEL
+    hipLaunchKernelGGL(MOSS_EX_PICK(k_expert_combine, WEIGHTS), dim3(grid), dim3(kExThreads), 0, st, p);
     MOSS_LAUNCH_CHECK();
     return MOSS_OK;
 }
@@ -336,16 +386,19 @@ extern "C" int moss_expert_plan(const int32_t *experts, int64_t tokens, int64_t 
     if (((uintptr_t)experts | (uintptr_t)row_of | (uintptr_t)source | (uintptr_t)offsets) & 3) return MOSS_ERR_ALIGN;
     int bits = 0;
     while ((1 << bits) < n_experts) bits++;
-    const size_t lds = (size_t)kPlanWaves * n_experts * 4;
+    const size_t lds = (size_t)(kPlanWaves + 2) * n_experts * 4;
     hipStream_t st = (hipStream_t)stream;
     if (lds > 48 * 1024) {
-        if (hipFuncSetAttribute((const void *)k_expert_plan, hipFuncAttributeMaxDynamicSharedMemorySize, kPlanWaves * kMaxExperts * 4) != hipSuccess) {
+        if (hipFuncSetAttribute((const void *)k_expert_plan, hipFuncAttributeMaxDynamicSharedMemorySize, (kPlanWaves + 2) * kMaxExperts * 4) != hipSuccess) {
             (void)hipGetLastError();
             return MOSS_ERR_HIP;
         }
     }
-    hipLaunchKernelGGL(k_expert_plan, dim3(1), dim3(kPlanThreads), lds, st, experts, tokens * k, (int)n_experts, bits, (int)multiple, rows,
-                       row_of, source, offsets);
+    // a thousand assignments each, but no more workgroups than it pays to count everything for
+    const int64_t n = tokens * k, wanted = (n + kPlanThreads - 1) / kPlanThreads, wgs = wanted < kPlanMaxWgs ? wanted : kPlanMaxWgs;
+    const int64_t part = (n + wgs - 1) / wgs;
+    hipLaunchKernelGGL(k_expert_plan, dim3((unsigned)((n + part - 1) / part)), dim3(kPlanThreads), lds, st, experts, n, (int)n_experts, bits, (int)multiple,
+                       rows, part, row_of, source, offsets);
     MOSS_LAUNCH_CHECK();
     return MOSS_OK;
 }
