@@ -108,6 +108,51 @@ __device__ __forceinline__ bool find_group_tile(GroupTile &t, const int32_t *off
     return false;
 }
 
+// Row tiles of the groups ahead of each, [groups + 1], by the first wave
+template <int BM>
+__device__ __forceinline__ void count_group_tiles(uint32_t *table, const int32_t *offsets, int groups, int64_t rows)
+{
+    const int lane = threadIdx.x & 63;
+    uint32_t before = 0;
+    for (int g0 = 0; g0 < groups; g0 += kWave) {
+        uint32_t n = 0;
+        if (g0 + lane < groups) {
+            int64_t first, end;
+            group_range(offsets, g0 + lane, rows, first, end);
+            n = (uint32_t)((end - first + BM - 1) / BM);
+        }
+        uint32_t upto = n;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) {
+            const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
+            if (lane >= d) upto += o;
+        }
+        if (g0 + lane < groups) table[g0 + lane] = before + upto - n;
+        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
+    }
+    if (lane == 0) table[groups] = before;
+}
+
+// The group of tile `at` among those that `table` counts, rows of tiles ahead of it and its own
+struct GroupTiles {
+    int group;
+    uint32_t ahead, count;
+};
+__device__ __forceinline__ GroupTiles group_of_tile(const uint32_t *table, int groups, uint32_t tiles_n, uint32_t at)
+{
+    const int lane = threadIdx.x & 63;
+    int g = 0;
+    for (int g0 = 0; g0 < groups; g0 += kWave) {      // groups that start at or ahead of this tile
+        const int o = g0 + lane;
+        g += __popcll(__ballot(o < groups && table[o < groups ? o : groups] * tiles_n <= at));
+    }
+    GroupTiles t;
+    t.group = __builtin_amdgcn_readfirstlane(g - 1);
+    t.ahead = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group]);
+    t.count = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group + 1]) - t.ahead;
+    return t;
+}
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 

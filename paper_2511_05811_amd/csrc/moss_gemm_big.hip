@@ -71,6 +71,8 @@ struct Frags {
 // its lanes' byte offsets for the global->LDS copies.
 struct TileCtx {
     int64_t m0, n0;
+    int64_t m_end;                               // rows of a end here (GROUP: those of the tile's group)
+    int group;
     const uint8_t *a_base, *b_base, *ae_base, *be_base;
     uint32_t a_off[8], b_off[8], ae_off, be_off;
 };
@@ -88,14 +90,23 @@ struct TileCtx {
 //    stages, which holds bytes of that row, so all lie inside the array (M * G % 4 == 0, host check).
 //  * The dword of the last stage, its lower 4 - t bytes zero, is put together ahead of the tile and kept, shifted by k, in
 //    a third scale slot, where it is read like the others.
-template <bool HAS_BE, int MI, bool RAGGED>
+//
+// GROUP: rows of a in groups, each with a matrix b and a scale of its own (moss_gemm_fp8_mx_grouped); the tiles of a group are its own.
+struct BigGroups {
+    const int32_t *offsets;
+    int groups;
+    int64_t ld_b, b_stride, b_s_stride;
+};
+struct BigNoGroups {};
+
+template <bool HAS_BE, int MI, bool RAGGED, bool GROUP>
 __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, int64_t K,
                                                         const uint8_t *__restrict__ a_q, const uint8_t *__restrict__ a_e,
                                                         const float *__restrict__ a_s,
                                                         const uint8_t *__restrict__ b_q, const uint8_t *__restrict__ b_e,
                                                         const float *__restrict__ b_s,
                                                         void *__restrict__ out, int out_f32, int64_t ld_out, int accumulate,
-                                                        int tiles_m, int tiles_n)
+                                                        int tiles_m, int tiles_n, std::conditional_t<GROUP, BigGroups, BigNoGroups> gr)
 {
     constexpr int kMT = MI * 64;             // rows of a per tile
     constexpr int kRowsA = kMT / 4;          // rows of a a wave copies per stage (64 or 32), in kPiecesA pieces of 8
@@ -114,8 +125,17 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
     const int tail_groups = G - 4 * (T - 1);                             // t (RAGGED: 1 .. 3)
     const int NB = RAGGED ? (T + 1) / 3 : (T + 3) >> 2;                  // scale blocks per tile (RAGGED: of stages 0 .. T - 2)
     const uint32_t kk = RAGGED ? (uint32_t)(i32 * G) & 3u : 0u;          // bytes by which this lane's exponent rows are off
-    const int total = tiles_m * tiles_n;
+    uint32_t *table = reinterpret_cast<uint32_t *>(big_smem + big_lds_bytes(false));       // GROUP: row tiles ahead of each group
+    int total = tiles_m * tiles_n;
+    int64_t ld_b = K;
+    if constexpr (GROUP) {
+        if (wave == 0) count_group_tiles<kMT>(table, gr.offsets, gr.groups, M);
+        __syncthreads();
+        total = __builtin_amdgcn_readfirstlane((int)table[gr.groups]) * tiles_n;
+        ld_b = gr.ld_b;
+    }
     const int n_my_tiles = (total - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x;
+    if (GROUP && (int)blockIdx.x >= total) return;
 
     // The k-th tile of this (persistent) workgroup.  Workgroups are dealt round-robin to the 8
     // XCDs (each with its own L2) and gridDim.x is a multiple of 8 whenever a workgroup has more
@@ -128,14 +148,25 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
             const int q = total >> 3, r = total & 7, xcd = pid & 7, idx = pid >> 3;
             pid = (xcd < r ? xcd * (q + 1) : r * (q + 1) + (xcd - r) * q) + idx;
         }
+        c.m0 = 0;
+        c.m_end = M;
+        c.group = 0;
+        int rows_of_tiles = tiles_m;
+        if constexpr (GROUP) {
+            const GroupTiles t = group_of_tile(table, gr.groups, (uint32_t)tiles_n, (uint32_t)pid);
+            c.group = t.group;
+            rows_of_tiles = (int)t.count;
+            pid -= (int)(t.ahead * (uint32_t)tiles_n);
+            group_range(gr.offsets, t.group, M, c.m0, c.m_end);
+        }
         constexpr int GM = 4;
         const int band = pid / (GM * tiles_n), rem = pid % (GM * tiles_n);
-        const int band_rows = (tiles_m - band * GM) < GM ? (tiles_m - band * GM) : GM;
+        const int band_rows = (rows_of_tiles - band * GM) < GM ? (rows_of_tiles - band * GM) : GM;
         // (the divisions run on the vector unit: tell the compiler the results are wave-uniform
         // so that everything derived from them lives in scalar registers)
         const int tm = __builtin_amdgcn_readfirstlane(band * GM + rem % band_rows);
         const int tn = __builtin_amdgcn_readfirstlane(rem / band_rows);
-        c.m0 = (int64_t)tm * kMT;
+        c.m0 += (int64_t)tm * kMT;
         c.n0 = (int64_t)tn * kBT;
         // per stage a wave copies kRowsA rows of a and 64 rows of b in wave-wide copies of 8 full rows
         // (8 x 128 B = 1 KiB of LDS) each; rows beyond the matrix repeat the last row.  In LDS a wave's
@@ -145,21 +176,22 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
             const int r = wave * 64 + s * 8 + (lane >> 3);
             const int ch = (lane & 7) ^ ((r >> 1) & 7);
             int64_t ra = c.m0 + wave * kRowsA + s * 8 + (lane >> 3), rb = c.n0 + r;
-            ra = (ra < M ? ra : M - 1) - c.m0;
+            ra = (ra < c.m_end ? ra : c.m_end - 1) - c.m0;
             rb = (rb < N ? rb : N - 1) - c.n0;
             c.a_off[s] = (uint32_t)(ra * K + ch * 16);
-            c.b_off[s] = (uint32_t)(rb * K + ch * 16);
+            c.b_off[s] = (uint32_t)(rb * ld_b + ch * 16);
         }
         {   // scale copies: lane = row, 16 of that row's exponent bytes
             const int r = wave * 64 + lane;
             int64_t ra = c.m0 + r, rb = c.n0 + r;
-            ra = (ra < M ? ra : M - 1) - c.m0;
+            ra = (ra < c.m_end ? ra : c.m_end - 1) - c.m0;
             rb = (rb < N ? rb : N - 1) - c.n0;
             c.ae_off = (uint32_t)(ra * G) & (RAGGED ? ~3u : ~0u);
             c.be_off = (uint32_t)(rb * G) & (RAGGED ? ~3u : ~0u);
         }
         c.a_base = a_q + c.m0 * K;
-        c.b_base = b_q + c.n0 * K;
+        c.b_base = b_q + c.n0 * ld_b;
+        if constexpr (GROUP) c.b_base += c.group * gr.b_stride;
         c.ae_base = a_e + c.m0 * G;
         c.be_base = HAS_BE ? b_e + c.n0 * G : nullptr;
     };
@@ -284,7 +316,7 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
     issue_stage(cx, 1, 1);
     if (RAGGED) prepare_tail(cx);
 
-    const float scale = (*a_s) * (*b_s);
+    float scale = GROUP ? 0.0f : (*a_s) * (*b_s);
 
     for (int ti = 0; ti < n_my_tiles; ti++) {
         const bool has_next = ti + 1 < n_my_tiles;
@@ -316,7 +348,8 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
         // copies of the stage after next and, in its second half, by the reads of the next stage's first fragments.  With one wave per SIMD a burst of memory
         // instructions would block this wave's issue -- and so the matrix pipe -- until the LDS /
         // texture queues had taken them all.
-        const int64_t m0 = cx.m0, n0 = cx.n0;
+        const int64_t m0 = cx.m0, n0 = cx.n0, m_end = cx.m_end;
+        if constexpr (GROUP) scale = (*a_s) * b_s[cx.group * gr.b_s_stride];
         for (int P = 0; P < T; P++) {
             const int par = (g0 + P) & 1;            // this stage's slot; the next stage sits in par ^ 1
             // Everything the middle of the stage and substep 1 need to know is worked out in the shadow of
@@ -463,7 +496,7 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
                     // (N % 8 == 0 and ld_out % 8 == 0 on this path: a piece is inside or outside as a whole)
                     // (streaming store: a BF16 output is an activation or gradient for a later layer, and leaving
                     // it out of the last-level cache keeps the operands of the GEMMs in flight there)
-                    if (m < M && n < N) st_stream16(o + m * ld_out + n, v);
+                    if (m < m_end && n < N) st_stream16(o + m * ld_out + n, v);
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // staged rows consumed before they are overwritten
             }
@@ -478,7 +511,7 @@ __global__ __launch_bounds__(256, 1) void k_gemm_mx_big(int64_t M, int64_t N, in
             for (int i = 0; i < MI; i++)
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    store_fragment(acc[i][j], scale, out, ld_out, mw + i * 32 + i32, nw + j * 32, h, M, N, true, accumulate);
+                    store_fragment(acc[i][j], scale, out, ld_out, mw + i * 32 + i32, nw + j * 32, h, m_end, N, true, accumulate);
         }
     }
     wait_vmcnt<0>();   // no copy into LDS may be outstanding when the wave ends
@@ -538,10 +571,10 @@ int moss_internal_gemm_big(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, 
     const int64_t tiles_m = narrow ? (M + kBT / 2 - 1) / (kBT / 2) : (M + kBT - 1) / kBT;
     if (tiles_m * tiles_n > 0x7FFFFFF) return MOSS_ERR_UNSUPPORTED;
     using Kern = void (*)(int64_t, int64_t, int64_t, const uint8_t *, const uint8_t *, const float *, const uint8_t *,
-                          const uint8_t *, const float *, void *, int, int64_t, int, int, int);
-    static const Kern kerns[8] = {k_gemm_mx_big<false, 4, false>, k_gemm_mx_big<true, 4, false>, k_gemm_mx_big<false, 2, false>,
-                                  k_gemm_mx_big<true, 2, false>,  k_gemm_mx_big<false, 4, true>, k_gemm_mx_big<true, 4, true>,
-                                  k_gemm_mx_big<false, 2, true>,  k_gemm_mx_big<true, 2, true>};
+                          const uint8_t *, const float *, void *, int, int64_t, int, int, int, BigNoGroups);
+    static const Kern kerns[8] = {k_gemm_mx_big<false, 4, false, false>, k_gemm_mx_big<true, 4, false, false>, k_gemm_mx_big<false, 2, false, false>,
+                                  k_gemm_mx_big<true, 2, false, false>,  k_gemm_mx_big<false, 4, true, false>, k_gemm_mx_big<true, 4, true, false>,
+                                  k_gemm_mx_big<false, 2, true, false>,  k_gemm_mx_big<true, 2, true, false>};
     static std::atomic<bool> attr_done[64][8];   // the LDS size attribute is set once per device and kernel (setting it
                                                  // twice from racing threads is harmless: same value)
     const int which = (b_e ? 1 : 0) | (narrow ? 2 : 0) | (ragged ? 4 : 0);
@@ -567,7 +600,42 @@ int moss_internal_gemm_big(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, 
     if (wgs > cus) wgs = cus;
     const dim3 grid((unsigned)(total < cus ? total : wgs)), block(256);
     hipLaunchKernelGGL(kerns[which], grid, block, big_lds_bytes(ragged), st, M, N, K, a_q, a_e, a_s, b_q, b_e, b_s, out, out_f32,
-                       ld_out, accumulate, (int)tiles_m, (int)tiles_n);
+                       ld_out, accumulate, (int)tiles_m, (int)tiles_n, BigNoGroups{});
+    if (hipGetLastError() != hipSuccess) return MOSS_ERR_HIP;
+    return MOSS_OK;
+}
+
+// Rows in groups: K of whole stages, outputs in whole 16-byte pieces, exponents of a; MOSS_ERR_UNSUPPORTED otherwise.
+bool moss_internal_gemm_big_groups_ok(int64_t N, int64_t K, const uint8_t *a_e, int64_t ld_out)
+{
+    return a_e && !((uintptr_t)a_e & 3) && K % 128 == 0 && K >= 512 && K <= (1 << 22) && N % 8 == 0 && ld_out % 8 == 0;
+}
+
+int moss_internal_gemm_big_groups(bool narrow, int64_t rows, int64_t N, int64_t K, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
+                                  const uint8_t *a_e, const float *a_s, const uint8_t *b_q, int64_t ld_b, int64_t b_stride, const float *b_s,
+                                  int64_t b_s_stride, void *out, int out_f32, int64_t ld_out, int accumulate, hipStream_t st)
+{
+    using namespace moss;
+    if (!moss_internal_gemm_big_groups_ok(N, K, a_e, ld_out)) return MOSS_ERR_UNSUPPORTED;
+    if ((int64_t)kBT * K >= ((int64_t)1 << 32) || (int64_t)kBT * ld_b >= ((int64_t)1 << 32)) return MOSS_ERR_UNSUPPORTED;
+    const int64_t bm = narrow ? kBT / 2 : kBT, tiles_n = (N + kBT - 1) / kBT, some = groups < rows ? groups : rows;
+    const int64_t most = (rows + some * (bm - 1)) / bm * tiles_n;        // every group ends in a tile of its own
+    if ((rows + bm - 1) / bm * groups * tiles_n > 0x7FFFFFF) return MOSS_ERR_UNSUPPORTED;      // (whatever the offsets are)
+    const auto kern = narrow ? k_gemm_mx_big<false, 2, false, true> : k_gemm_mx_big<false, 4, false, true>;
+    const int lds = big_lds_bytes(false) + ((int)groups + 1) * 4;
+    static std::atomic<bool> attr_done[64][2];
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOSS_ERR_HIP;
+    if (!attr_done[dev][narrow].load()) {
+        if (hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != hipSuccess) {
+            (void)hipGetLastError();
+            return MOSS_ERR_UNSUPPORTED;
+        }
+        attr_done[dev][narrow].store(true);
+    }
+    const int cus = big_cus();
+    hipLaunchKernelGGL(kern, dim3((unsigned)(most < cus ? most : cus)), dim3(256), lds, st, rows, N, K, a_q, a_e, a_s, b_q, (const uint8_t *)nullptr, b_s,
+                       out, out_f32, ld_out, accumulate, 0, (int)tiles_n, BigGroups{offsets, (int)groups, ld_b, b_stride, b_s_stride});
     if (hipGetLastError() != hipSuccess) return MOSS_ERR_HIP;
     return MOSS_OK;
 }

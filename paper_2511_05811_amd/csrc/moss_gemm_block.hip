@@ -8,7 +8,18 @@
 
 namespace {
 
-enum BlockKind { kBlockSmall, kBlockHalf, kBlockWide };
+enum BlockKind { kBlockSmall, kBlock64, kBlock128, kBlockHalf, kBlockWide };
+
+template <moss::WideForm FORM>
+int launch_block(int kind, const moss::WideArgs &p, hipStream_t st)
+{
+    switch (kind) {
+        case kBlock64: return moss::launch_wide<FORM, 2, 2, 5>(p, st);
+        case kBlock128: return moss::launch_wide<FORM, 4, 2, 4>(p, st);
+        case kBlockHalf: return moss::launch_wide<FORM, 4, 4, 3>(p, st);
+        default: return moss::launch_wide<FORM, 8, 4, 2>(p, st);
+    }
+}
 
 int moss_block_kind(int64_t M, int64_t N, int64_t K, bool, int64_t ld_out)
 {
@@ -43,8 +54,7 @@ extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uin
         p.end_b = (N + b_block - 1) / b_block * 4 * blocks;
         p.ld_b = K;
         p.out = out; p.ld_out = ld_out; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
-        const int rc = b_block == 1 ? (kind == kBlockWide ? launch_wide<kWideBlockRows, 8, 2>(p, st) : launch_wide<kWideBlockRows, 4, 3>(p, st))
-                                    : (kind == kBlockWide ? launch_wide<kWideBlock, 8, 2>(p, st) : launch_wide<kWideBlock, 4, 3>(p, st));
+        const int rc = b_block == 1 ? launch_block<kWideBlockRows>(kind, p, st) : launch_block<kWideBlock>(kind, p, st);
         if (rc != MOSS_ERR_UNSUPPORTED) return rc;
     }
     MidArgs p{};

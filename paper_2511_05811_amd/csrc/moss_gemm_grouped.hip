@@ -19,13 +19,14 @@ int check_common(int64_t rows, int64_t groups, const int32_t *offsets, int out_d
     return ((uintptr_t)offsets & 3) ? MOSS_ERR_ALIGN : MOSS_OK;
 }
 
-// Tiles: 0 .. 4 the small ones, then 128 x 256 and 256 x 256 of the wide kernel
-enum { kHalf = 5, kWide = 6 };
+// Tiles: 0 .. 4 the small ones, then 128 x 256 and 256 x 256 of the wide kernel and of the large-tile kernel
+enum { kHalf = 5, kWide = 6, kLargeHalf = 7, kLarge = 8 };
 
-int rows_kind(int64_t rows, int64_t N, int64_t K, int64_t groups, bool a_e, int64_t ld_out)
+int rows_kind(int64_t rows, int64_t N, int64_t K, int64_t groups, const uint8_t *a_e, int64_t ld_out)
 {
     const int64_t avg = (rows + groups - 1) / groups;
     if (!a_e || K < 128 || N % 8 || ld_out % 8 || avg <= 128) return avg <= 32 ? 0 : avg <= 64 ? 1 : avg <= 128 ? 2 : 3;
+    if (moss_internal_gemm_big_groups_ok(N, K, a_e, ld_out)) return avg <= 256 ? kLargeHalf : kLarge;
     return avg <= 256 ? kHalf : kWide;
 }
 
@@ -52,7 +53,12 @@ extern "C" int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int6
     if (!moss_aligned16(a_q) || !moss_aligned16(b_q) || !moss_aligned16(out) || ld_b % 16 || b_stride % 16) return MOSS_ERR_ALIGN;
     if (((uintptr_t)a_e & 3) || ((uintptr_t)a_s & 3) || ((uintptr_t)b_s & 3)) return MOSS_ERR_ALIGN;
     hipStream_t st = (hipStream_t)stream;
-    const int kind = rows_kind(rows, N, K, groups, a_e != nullptr, ld_out);
+    const int kind = rows_kind(rows, N, K, groups, a_e, ld_out);
+    if (kind >= kLargeHalf) {
+        const int rc = moss_internal_gemm_big_groups(kind == kLargeHalf, rows, N, K, groups, offsets, a_q, a_e, a_s, b_q, ld_b, b_stride, b_s, b_s_stride,
+                                                     out, out_dtype == MOSS_DT_F32, ld_out, accumulate, st);
+        if (rc != MOSS_ERR_UNSUPPORTED) return rc;
+    }
     if (kind >= kHalf) {
         WideArgs p{};
         p.M = rows; p.N = N; p.K = K;
@@ -63,7 +69,7 @@ extern "C" int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int6
         p.ld_b = ld_b; p.b_stride = b_stride; p.b_s_stride = b_s_stride;
         p.offsets = offsets; p.groups = (int)groups;
         p.out = out; p.ld_out = ld_out; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
-        const int rc = kind == kWide ? launch_wide<kWideGroupRows, 8, 2>(p, st) : launch_wide<kWideGroupRows, 4, 3>(p, st);
+        const int rc = kind == kWide ? launch_wide<kWideGroupRows, 8, 4, 2>(p, st) : launch_wide<kWideGroupRows, 4, 4, 3>(p, st);
         if (rc != MOSS_ERR_UNSUPPORTED) return rc;
     }
     MidGroupArgs p{};
@@ -102,7 +108,7 @@ extern "C" int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, i
         p.ld_b = rows;
         p.offsets = offsets; p.groups = (int)groups;
         p.out = out; p.ld_out = N; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
-        const int rc = kind == kWide ? launch_wide<kWideGroupDw, 8, 2>(p, st) : launch_wide<kWideGroupDw, 4, 3>(p, st);
+        const int rc = kind == kWide ? launch_wide<kWideGroupDw, 8, 4, 2>(p, st) : launch_wide<kWideGroupDw, 4, 4, 3>(p, st);
         if (rc != MOSS_ERR_UNSUPPORTED) return rc;
     }
     MidGroupArgs p{};

@@ -1,7 +1,7 @@
 // Wide-tile FP8 GEMM for the products of experts and for operands with an FP32 scale per block of 128.
 //
 // Shape of the kernel
-//  * (32 MI) x 256 outputs per workgroup of 8 waves (2 x 4), two waves per SIMD, (16 MI) x 64 per wave in 16 x 16 accumulators of
+//  * (32 MI) x (64 NJ) outputs per workgroup of 8 waves (2 x 4), two waves per SIMD, (16 MI) x (16 NJ) per wave in 16 x 16 accumulators of
 //    V_MFMA_(SCALE_)F32_16X16X128_F8F6F4, all of them vector registers: the blocked forms add to them on the vector unit.  One
 //    matrix instruction covers a stage of K = 128, which is a block.
 //  * Stages go through SLOTS slots of LDS, filled by direct global->LDS copies of 128 bytes per row.  One barrier per stage, behind the
@@ -52,18 +52,18 @@ struct WideArgs {
 extern __shared__ __attribute__((aligned(1024))) uint8_t wide_smem[];
 
 constexpr int kWideThreads = 512;
-constexpr int kWideBN = 256;
 constexpr int kWideK = 128;
 
-template <int MI, int SLOTS>
+template <int MI, int NJ, int SLOTS>
 struct WideShape {
-    static constexpr int kBM = 32 * MI;
-    static constexpr int kRows = kBM + kWideBN;
+    static constexpr int kBM = 32 * MI, kBN = 64 * NJ;
+    static constexpr int kRows = kBM + kBN;
     static constexpr int kSlot = kRows * kWideK;
     static constexpr int kPieces = kRows / 8 / 8;               // 8-row copies per wave and stage
     static constexpr int kRing = SLOTS * kSlot;                 // [2 blocks][4 stages][rows] dwords
     static constexpr int kTable = kRing + 8 * kRows * 4;        // tiles ahead of each group (kWideGroupRows)
-    static_assert(kRows % 64 == 0 && kBM % 16 == 0, "whole copies per wave");
+    static_assert(kBM % 64 == 0 && kBN % 64 == 0, "whole copies per wave, whole waves of rows");
+    static_assert(MI * NJ % 4 == 0 && MI % 2 == 0, "parts and fragments take turns from stage to stage");
     static constexpr int lds_bytes(WideForm form, int groups) { return kTable + (form == kWideGroupRows ? (groups + 1) * 4 : 0); }
 };
 
@@ -126,35 +126,11 @@ __host__ __device__ __forceinline__ uint32_t eighths_of(uint32_t each, uint32_t 
     return n;
 }
 
-// Row tiles of the groups ahead of each, [groups + 1], by the first wave
-template <int BM>
-__device__ __forceinline__ void count_group_tiles(uint32_t *table, const int32_t *offsets, int groups, int64_t rows)
-{
-    const int lane = threadIdx.x & 63;
-    uint32_t before = 0;
-    for (int g0 = 0; g0 < groups; g0 += kWave) {
-        uint32_t n = 0;
-        if (g0 + lane < groups) {
-            int64_t first, end;
-            group_range(offsets, g0 + lane, rows, first, end);
-            n = (uint32_t)((end - first + BM - 1) / BM);
-        }
-        uint32_t upto = n;
-#pragma unroll
-        for (int d = 1; d < kWave; d <<= 1) {
-            const uint32_t o = (uint32_t)__shfl_up((int)upto, d, 64);
-            if (lane >= d) upto += o;
-        }
-        if (g0 + lane < groups) table[g0 + lane] = before + upto - n;
-        before += (uint32_t)__builtin_amdgcn_readlane((int)upto, 63);
-    }
-    if (lane == 0) table[groups] = before;
-}
-
-template <WideForm FORM, int MI, int SLOTS>
+template <WideForm FORM, int MI, int NJ, int SLOTS>
 __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
 {
-    using S = WideShape<MI, SLOTS>;
+    using S = WideShape<MI, NJ, SLOTS>;
+    constexpr int kWideBN = S::kBN;
     constexpr bool kBlocked = FORM == kWideBlock || FORM == kWideBlockRows;
     constexpr int kBM = S::kBM, kPieces = S::kPieces;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
@@ -201,15 +177,10 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         t.first = 0;
         t.end = p.K;
         if constexpr (FORM == kWideGroupRows) {
-            int g = 0;
-            for (int g0 = 0; g0 < p.groups; g0 += kWave) {       // groups that start at or ahead of this tile
-                const int o = g0 + lane;
-                g += __popcll(__ballot(o < p.groups && table[o < p.groups ? o : p.groups] * (uint32_t)p.tiles_n <= at));
-            }
-            t.group = __builtin_amdgcn_readfirstlane(g - 1);
-            const uint32_t ahead = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group]);
-            tiles_m = (uint32_t)__builtin_amdgcn_readfirstlane((int)table[t.group + 1]) - ahead;
-            at -= ahead * (uint32_t)p.tiles_n;
+            const GroupTiles of = group_of_tile(table, p.groups, (uint32_t)p.tiles_n, at);
+            t.group = of.group;
+            tiles_m = of.count;
+            at -= of.ahead * (uint32_t)p.tiles_n;
             group_range(p.offsets, t.group, p.M, t.m0, t.rows_end);
         }
         if constexpr (FORM == kWideGroupDw) {
@@ -293,7 +264,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         if (!kBlocked) s_back = (uint32_t)((begin + (int64_t)(t.T - 1) * kWideK - stage_at(t, t.T - 1)) >> 5);
         if (!s_there) return;
         const int64_t row0 = s_is_a ? t.m0 : FORM == kWideBlock ? t.n0 >> 7 : t.n0, pitch = s_is_a ? p.pitch_a : p.pitch_b;
-        const int last = (int)((s_is_a ? t.rows_end - t.m0 : p.N - t.n0) < 256 ? (s_is_a ? t.rows_end - t.m0 : p.N - t.n0) : 256) - 1;
+        const int last = (int)((s_is_a ? t.rows_end - t.m0 : p.N - t.n0) < S::kRows ? (s_is_a ? t.rows_end - t.m0 : p.N - t.n0) : S::kRows) - 1;
         int r = s_is_a ? tid : tid - kBM;
         r = r < last ? r : last;
         if (FORM == kWideBlock && !s_is_a) r >>= 7;
@@ -333,13 +304,13 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     };
 
     // ---- what is computed
-    v4f acc[MI][4], part[kBlocked ? 4 : 1];
-    v8i fa[2], fb[4];
-    uint32_t sa[4] = {0, 0, 0, 0}, sb[4];            // exponent bytes (sb: of each fragment); scales of rows of a, of blocks of b
-    float row_scale[FORM == kWideBlockRows ? 4 : 1][4], both[2];
+    v4f acc[MI][NJ], part[kBlocked ? 4 : 1];
+    v8i fa[2], fb[NJ];
+    uint32_t sa[4] = {0, 0, 0, 0}, sb[NJ];           // exponent bytes (sb: of each fragment); scales of rows of a, of blocks of b
+    float row_scale[FORM == kWideBlockRows ? NJ : 1][4], both[2];
     const int sw = (r16 >> 1) & 7;
     const uint32_t lane_at = (uint32_t)(r16 * kWideK + ((q ^ sw) << 4));
-    const uint32_t a_at = lane_at + (uint32_t)(wm * 16 * MI * kWideK), b_at = lane_at + (uint32_t)((kBM + wn * 64) * kWideK);
+    const uint32_t a_at = lane_at + (uint32_t)(wm * 16 * MI * kWideK), b_at = lane_at + (uint32_t)((kBM + wn * 16 * NJ) * kWideK);
     // (chunk q + 4 of a row lies 64 bytes from chunk q, whichever way)
     auto read_fragment = [&](v8i &f, uint32_t at, uint32_t at64) {
         const uint4 lo = *reinterpret_cast<const uint4 *>(wide_smem + at), hi = *reinterpret_cast<const uint4 *>(wide_smem + at64);
@@ -353,9 +324,9 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     };
     auto read_b = [&](int j, uint32_t slot) { read_fragment(fb[j], b_at + slot + (uint32_t)(j * 16 * kWideK), (b_at ^ 64) + slot + (uint32_t)(j * 16 * kWideK)); };
     auto read_b_scale = [&](int j, int stage) {
-        const uint32_t *x = ring + stage * S::kRows + kBM + wn * 64 + j * 16;
+        const uint32_t *x = ring + stage * S::kRows + kBM + wn * 16 * NJ + j * 16;
         if (FORM == kWideBlock) {
-            if (j == 0) sb[0] = x[0];                            // (64 columns share it)
+            if (j == 0) sb[0] = x[0];                            // (a wave's columns share it)
         } else if (FORM == kWideBlockRows) {
             const float4 v = *reinterpret_cast<const float4 *>(x + 4 * q);
             row_scale[FORM == kWideBlockRows ? j : 0][0] = v.x; row_scale[FORM == kWideBlockRows ? j : 0][1] = v.y;
@@ -366,8 +337,11 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
             sb[j] = 127;
         }
     };
-    auto fold = [&](int i, int j) {
-        v4f &d = part[kBlocked ? j : 0];
+    // instruction number n of a stage is that of fragments (n / NJ, n % NJ); its part is n % 4
+    constexpr int kAll = MI * NJ;
+    auto fold = [&](int n) {
+        const int i = n / NJ, j = n % NJ;
+        v4f &d = part[kBlocked ? n & 3 : 0];
         asm volatile("" : "+v"(d));
 #pragma unroll
         for (int v = 0; v < 4; v++) {
@@ -396,7 +370,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     uint32_t slot = 0;
     read_a(0, 0, 0);
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
+    for (int j = 0; j < NJ; j++) {
         read_b(j, 0);
         read_b_scale(j, 0);
     }
@@ -406,7 +380,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
 #pragma unroll
         for (int i = 0; i < MI; i++)
 #pragma unroll
-            for (int j = 0; j < 4; j++)
+            for (int j = 0; j < NJ; j++)
 #pragma unroll
                 for (int v = 0; v < 4; v++) acc[i][j][v] = 0.0f;
         if (kBlocked) {
@@ -440,31 +414,33 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
                 }
                 if (!kBlocked) {
                     // vector ALU write (the byte of the exponent) -> operand of a matrix instruction
-                    if (i == 0) asm volatile("" : "+v"(sb[0]), "+v"(sb[1]), "+v"(sb[2]), "+v"(sb[3]));
+                    if (i == 0)
+#pragma unroll
+                        for (int j = 0; j < NJ; j++) asm volatile("" : "+v"(sb[j]));
                     asm volatile("s_nop 4" : "+v"(sa[i & 3]));
                 }
                 if (FORM == kWideBlock) both[i & 1] = block_scales(__uint_as_float(sa[i & 3]), __uint_as_float(sb[0]));
 #pragma unroll
-                for (int j = 0; j < 4; j++) {
-                    if (kBlocked) mfma16_from_zero(part[kBlocked ? j : 0], fb[j], fa[i & 1]);
+                for (int j = 0; j < NJ; j++) {
+                    if (kBlocked) mfma16_from_zero(part[kBlocked ? (i * NJ + j) & 3 : 0], fb[j], fa[i & 1]);
                     else mfma16_scaled(acc[i][j], fb[j], fa[i & 1], sb[j], sa[i & 3]);
                     if (kBlocked) {
-                        if (j >= 2) {
-                            fold(i, j - 2);
-                            if (i == MI - 1 && FORM == kWideBlockRows) read_b_scale(j - 2, next_stage);
-                        } else {
-                            fold((i + MI - 1) % MI, j + 2);
-                            if (i == 0 && FORM == kWideBlockRows) read_b_scale(j + 2, stage);
-                        }
+                        // (the last two of a stage are folded in the next one.  The scales of the next stage's rows of b are read
+                        // when those of this one have been used)
+                        const int n = i * NJ + j - 2, of = n >= 0 ? n : n + kAll;
+                        fold(of);
+                        if (of / NJ == MI - 1 && FORM == kWideBlockRows) read_b_scale(of % NJ, n >= 0 ? next_stage : stage);
                     }
-                    if (i + 1 < MI && j == 0) read_a(i + 1, slot, stage);
+                    // (with two fragments of a, the scale of the one ahead is used for the last time by this one's second fold)
+                    constexpr int kReadA = FORM == kWideBlockRows && MI == 2 ? 1 : 0;
+                    if (i + 1 < MI && j == kReadA) read_a(i + 1, slot, stage);
                     if (i == MI - 1) {
-                        if (j == 0) read_a(0, next_slot, next_stage);
+                        if (j == kReadA) read_a(0, next_slot, next_stage);
                         read_b(j, next_slot);
                         if (FORM != kWideBlockRows) read_b_scale(j, next_stage);
                         if (copies)
 #pragma unroll
-                            for (int x = j * kPieces / 4; x < (j + 1) * kPieces / 4; x++) copy_piece(x);
+                            for (int x = j * kPieces / NJ; x < (j + 1) * kPieces / NJ; x++) copy_piece(x);
                     }
                     pin();
                 }
@@ -486,35 +462,39 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         float scale = 1.0f;
         if (kBlocked) {
             asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last matrix instructions retire
-            fold(MI - 1, 2);
-            fold(MI - 1, 3);
+            fold(kAll - 2);
+            fold(kAll - 1);
         } else {
             scale = *p.a_s * p.b_s[FORM == kWideGroupRows ? t.group * p.b_s_stride : 0];
             asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
 #pragma unroll
             for (int i = 0; i < MI; i++)
 #pragma unroll
-                for (int j = 0; j < 4; j++) asm volatile("" : "+v"(acc[i][j]));
+                for (int j = 0; j < NJ; j++) asm volatile("" : "+v"(acc[i][j]));
         }
         void *out = p.out;
         if (FORM == kWideGroupDw) out = (uint8_t *)p.out + (int64_t)t.group * p.M * p.ld_out * (p.out_f32 ? 4 : 2);
 #pragma unroll
         for (int i = 0; i < MI; i++)
 #pragma unroll
-            for (int j = 0; j < 4; j += 2)
-                store_pair(acc[i][j], acc[i][j + 1], scale, out, p.ld_out, t.m0 + wm * 16 * MI + i * 16 + r16, t.n0 + wn * 64 + j * 16, q, t.rows_end, p.N,
+            for (int j = 0; j < NJ; j += 2)
+                store_pair(acc[i][j], acc[i][j + 1], scale, out, p.ld_out, t.m0 + wm * 16 * MI + i * 16 + r16, t.n0 + wn * 16 * NJ + j * 16, q, t.rows_end, p.N,
                            p.out_f32, p.accumulate);
     }
     wait_vmcnt<0>();   // no copy into LDS may be outstanding when the wave ends
 }
 
-template <WideForm FORM, int MI, int SLOTS>
+template <WideForm FORM, int MI, int NJ, int SLOTS>
 static int launch_wide(WideArgs p, hipStream_t st)
 {
-    using S = WideShape<MI, SLOTS>;
+    using S = WideShape<MI, NJ, SLOTS>;
+    // a stage lies inside a row, outputs are whole 16-byte pieces, offsets inside a tile have 32 bits
+    constexpr int64_t kMaxLd = (int64_t)1 << 24;
+    if (p.K < kWideK || p.K % kGroup || p.N % 8 || p.ld_out % 8 || p.K > kMaxLd || p.ld_b > kMaxLd || !p.a_x) return MOSS_ERR_UNSUPPORTED;
+    if (S::lds_bytes(FORM, p.groups) > 160 * 1024) return MOSS_ERR_UNSUPPORTED;
     int cus = moss_internal_cu_count();
     cus = cus <= 0 ? 256 : cus >= 8 ? cus & ~7 : 8;
-    const int64_t tiles_n = (p.N + kWideBN - 1) / kWideBN;
+    const int64_t tiles_n = (p.N + S::kBN - 1) / S::kBN;
     int64_t tiles_m = (p.M + S::kBM - 1) / S::kBM, total = tiles_m * tiles_n;
     int64_t most = total;
     if (FORM == kWideGroupRows) {
@@ -534,7 +514,7 @@ static int launch_wide(WideArgs p, hipStream_t st)
     }
     p.tiles_m = (int)tiles_m;
     p.tiles_n = (int)tiles_n;
-    const auto kern = k_gemm_wide<FORM, MI, SLOTS>;
+    const auto kern = k_gemm_wide<FORM, MI, NJ, SLOTS>;
     static std::atomic<bool> attr_set[64];           // per device: the LDS size it may ask for has been raised
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOSS_ERR_HIP;

@@ -47,6 +47,12 @@ bool moss_internal_gemm_big_ragged_ok(int64_t M, int64_t N, int64_t K, const uin
 bool moss_internal_gemm_big_ragged(int64_t M, int64_t N, int64_t K, const uint8_t *a_e, const uint8_t *b_e, int accumulate,
                                    int64_t ld_out);
 
+// the same for rows in groups (moss_gemm_fp8_mx_grouped), in tiles of 256 or (narrow) 128 rows
+bool moss_internal_gemm_big_groups_ok(int64_t N, int64_t K, const uint8_t *a_e, int64_t ld_out);
+int moss_internal_gemm_big_groups(bool narrow, int64_t rows, int64_t N, int64_t K, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
+                                  const uint8_t *a_e, const float *a_s, const uint8_t *b_q, int64_t ld_b, int64_t b_stride, const float *b_s,
+                                  int64_t b_s_stride, void *out, int out_f32, int64_t ld_out, int accumulate, hipStream_t st);
+
 // small tiles and split K for problems that leave the large tiles idle, and ragged K: the kind of tiles, or -1 if another kernel
 // is the better choice; MOSS_ERR_UNSUPPORTED if the device cannot launch them
 int moss_internal_gemm_mid_kind(int64_t M, int64_t N, int64_t K, const uint8_t *a_e, const uint8_t *b_e, int accumulate,
