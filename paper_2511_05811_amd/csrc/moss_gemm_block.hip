@@ -2,13 +2,54 @@
 // MOSS is compared with, paper Sec. 1 and 3.1):
 //      out[m, n] (+)= sum_kb a_s[m, kb] b_s[n or n / 128, kb] sum_{k in kb} dec(a[m, k]) dec(b[n, k]).
 // The scales cannot leave the main loop: the sum of every block is taken from zero by the matrix unit and added to the accumulators
-// times both scales by the vector unit.  Kernel: the small tiles, whose stage is one block (moss_gemm_mid.h).
+// times both scales by the vector unit.  Kernels: the wide tiles (moss_gemm_wide.h) and, where few rows leave them idle and for what they
+// cannot take, the small tiles with K split over the waves (moss_gemm_mid.h); a stage is one block in both.
+//
+// Bound, large products: power.  8192 x 11008 x 4096 takes 399 us (1.85 PFLOP/s) on quantized data and 511 on random codes, and neither
+// the waits nor the barriers left out shorten it; the copies are 18 % of it, the additions on the vector unit 11 %, the stores 8 %.
+// (The MOSS product of the same size, whose scales the matrix instruction applies: 322 us.)  Few rows: the weight's bytes, 17 x 11008 x
+// 4096 10.4 us, 4.4 TB/s.
 #include "moss_gemm_mid.h"
 #include "moss_gemm_wide.h"
 
 namespace {
 
 enum BlockKind { kBlockSmall, kBlock64, kBlock128, kBlockHalf, kBlockWide };
+
+// Fits to 400 random products (M 1 to 16384, N 256 to 11008, K 32 to 8192; a scale per 128 rows of b, or per row), each run in every
+// kind of tiles: the kind chosen took 0.5 % (1.0 %) more than the fastest of its problem.  us, a scale per
+// 128 rows of b, 32 x 32 / 64 x 128 / 128 x 128 / 128 x 256 / 256 x 256:
+//     98 x 3840 x 2944     7.3 / 16.6 / 20.2 / 26.6 / 41.0      512 x 4096 x 4096    31.5 / 23.3 / 27.4 / 36.6 / 57.5
+//     1086 x 640 x 640     7.4 /  7.4 /  8.6 / 10.7 / 15.6      651 x 4032 x 1216    26.3 / 17.9 / 13.2 / 16.7 / 24.8
+//     4553 x 1792 x 2048  80.1 / 45.3 / 31.7 / 26.1 / 36.4      8192 x 11008 x 4096    - /  970 /  618 /  477 /  418
+// and per row: 384 x 1664 x 6688 28.2 / 36.5 / 47.4 / 73.1 / 120, 1280 x 2048 x 2944 35.7 / 34.4 / 25.5 / 34.3 / 52.2,
+// 4096 x 4096 x 2016 202 / 93.3 / 66.9 / 57.9 / 51.1.
+constexpr MossTileCost kCost[2][5] = {{{2.2, 0.73, 0.52, 0.89, 0.12, 32, 32, 4, 2, false},
+                                       {4.0, 0.18, 0.53, 1.43, 0.04, 64, 128, 1, 1, true},
+                                       {4.5, 0.0, 0.67, 2.19, 0.02, 128, 128, 1, 1, true},
+                                       {4.8, 0.0, 0.95, 4.36, 0.03, 128, 256, 1, 1, true},
+                                       {5.7, 0.0, 1.56, 8.5, 0.04, 256, 256, 1, 1, true}},
+                                      {{2.5, 0.0, 0.78, 1.07, 0.21, 32, 32, 4, 2, false},
+                                       {3.6, 0.87, 0.57, 1.03, 0.02, 64, 128, 1, 1, true},
+                                       {3.8, 0.99, 0.79, 1.82, 0.01, 128, 128, 1, 1, true},
+                                       {4.3, 1.14, 1.19, 3.26, 0.03, 128, 256, 1, 1, true},
+                                       {7.3, 0.0, 1.9, 6.9, 0.04, 256, 256, 1, 1, true}}};
+
+int block_kind(int64_t M, int64_t N, int64_t K, int64_t b_block, int64_t ld_out)
+{
+    if (K < 128 || N % 8 || ld_out % 8) return kBlockSmall;       // (what the wide tiles cannot take)
+    int best = 0;
+    double least = 0.0;
+    for (int k = 0; k < 5; k++) {
+        const MossTileCost &c = kCost[b_block == 1][k];
+        const double us = moss_tile_us(c, (double)moss_ceil_div(M, c.bm) * (double)moss_ceil_div(N, c.bn), (double)moss_ceil_div(K, 128 * c.k_groups), K % 128 != 0);
+        if (k == 0 || us < least) {
+            best = k;
+            least = us;
+        }
+    }
+    return best;
+}
 
 template <moss::WideForm FORM>
 int launch_block(int kind, const moss::WideArgs &p, hipStream_t st)
@@ -21,14 +62,14 @@ int launch_block(int kind, const moss::WideArgs &p, hipStream_t st)
     }
 }
 
-int moss_block_kind(int64_t M, int64_t N, int64_t K, bool, int64_t ld_out)
-{
-    if (K < 128 || N % 8 || ld_out % 8) return kBlockSmall;
-    if (M * N < 512 * 512) return kBlockSmall;
-    return M * N >= 2048 * 4096 ? kBlockWide : kBlockHalf;
-}
-
 }  // namespace
+
+// The tile (rows * 1000 + columns) that a product takes (the tests hold the choice by it)
+extern "C" int moss_internal_gemm_block_tile(int64_t M, int64_t N, int64_t K, int64_t b_block, int64_t ld_out)
+{
+    const MossTileCost &c = kCost[0][block_kind(M, N, K, b_block, ld_out)];
+    return c.bm * 1000 + c.bn;
+}
 
 extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, const float *a_s, const uint8_t *b_q,
                                       const float *b_s, int64_t b_block, void *out, int out_dtype, int64_t ld_out, int accumulate, void *stream)
@@ -43,7 +84,7 @@ extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uin
     if (K > ((int64_t)1 << 22)) return MOSS_ERR_UNSUPPORTED;      // 32-bit offsets inside a tile
     hipStream_t st = (hipStream_t)stream;
     const int64_t blocks = (K + 127) / 128;
-    const int kind = moss_block_kind(M, N, K, out_dtype == MOSS_DT_F32, ld_out);
+    const int kind = block_kind(M, N, K, b_block, ld_out);
     if (kind != kBlockSmall) {
         WideArgs p{};
         p.M = M; p.N = N; p.K = K;
@@ -63,5 +104,5 @@ extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uin
     p.b_q = b_q; p.b_e = (const uint8_t *)b_s;
     p.out = out; p.ld_out = ld_out; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
     p.e_dwords = 1;
-    return b_block == 1 ? launch_mid_kind<kMidBlockRows>(0, p, st) : launch_mid_kind<kMidBlock>(0, p, st);
+    return b_block == 1 ? launch_mid_kind<kMidBlockRows, 0>(p, st) : launch_mid_kind<kMidBlock, 0>(p, st);
 }

@@ -623,17 +623,15 @@ static int launch_mid(MidArgsOf<FORM> p, int budget, hipStream_t st)
     return MOSS_OK;
 }
 
-template <MidForm FORM>
-static int launch_mid_kind(int kind, const MidArgsOf<FORM> &p, hipStream_t st)
+// The kinds of tiles, smallest first
+template <MidForm FORM, int KIND>
+static int launch_mid_kind(const MidArgsOf<FORM> &p, hipStream_t st)
 {
-    if constexpr (FORM == kMidBlock || FORM == kMidBlockRows) return launch_mid<FORM, 1, 1, 1, 1, 4, 2>(p, 80 * 1024, st);
-    else switch (kind) {
-        case 0: return launch_mid<FORM, 1, 1, 1, 1, 4, 2>(p, 80 * 1024, st);       // two workgroups fit a compute unit
-        case 1: return launch_mid<FORM, 2, 2, 1, 1, 4, 2>(p, 160 * 1024, st);
-        case 2: return launch_mid<FORM, 2, 2, 1, 2, 2, 3>(p, 160 * 1024, st);
-        case 3: return launch_mid<FORM, 2, 2, 2, 2, 1, 4>(p, 160 * 1024, st);
-        default: return launch_mid<FORM, 2, 3, 2, 2, 1, 3>(p, 160 * 1024, st);
-    }
+    if constexpr (KIND == 0) return launch_mid<FORM, 1, 1, 1, 1, 4, 2>(p, 80 * 1024, st);       // two workgroups fit a compute unit
+    else if constexpr (KIND == 1) return launch_mid<FORM, 2, 2, 1, 1, 4, 2>(p, 160 * 1024, st);
+    else if constexpr (KIND == 2) return launch_mid<FORM, 2, 2, 1, 2, 2, 3>(p, 160 * 1024, st);
+    else if constexpr (KIND == 3) return launch_mid<FORM, 2, 2, 2, 2, 1, 4>(p, 160 * 1024, st);
+    else return launch_mid<FORM, 2, 3, 2, 2, 1, 3>(p, 160 * 1024, st);
 }
 
 }  // namespace moss

@@ -139,5 +139,11 @@ int moss_internal_gemm_mid(int kind, int64_t M, int64_t N, int64_t K, const uint
     p.b_q = b_q; p.b_e = b_e; p.b_s = b_s;
     p.out = out; p.ld_out = ld_out; p.out_f32 = out_f32; p.accumulate = accumulate;
     p.e_dwords = K % 128 == 0;
-    return launch_mid_kind<kMidDense>(kind, p, st);
+    switch (kind) {
+        case 0: return launch_mid_kind<kMidDense, 0>(p, st);
+        case 1: return launch_mid_kind<kMidDense, 1>(p, st);
+        case 2: return launch_mid_kind<kMidDense, 2>(p, st);
+        case 3: return launch_mid_kind<kMidDense, 3>(p, st);
+        default: return launch_mid_kind<kMidDense, 4>(p, st);
+    }
 }

@@ -12,13 +12,14 @@
 //    times its scales when two further instructions have been issued; the matrix unit takes them one after the other, so it has
 //    retired by then.  This order is all that protects the read; the instructions are volatile asm and a part passes through an
 //    empty one at that place.
-//  * Exponents (four bytes) or scales (a float) of a stage are one dword per row.  A thread fetches those of its row for four stages ahead
-//    into registers and leaves them in a ring in LDS at the end of the four before.
+//  * Exponents (four bytes) or scales (a float) of a stage are one dword per row.  A thread fetches those of its row for a block of stages
+//    ahead into registers and leaves them in a ring in LDS at the end of the block before.
 //  * Persistent workgroups walk their tiles in one stream of stages: copies and scales of the next tile are on their way while this one
 //    ends.  Three places in that stream are kept: what is computed, what is copied (SLOTS stages ahead) and what is
-//    scaled (a block of four ahead).
-//  * K that ends inside a stage, groups of rows of any length: the last stage's copies are moved back to end with the row, and what of
-//    a stage does not belong to the sum is zeroed in the fragments of a.
+//    scaled (a block of stages ahead).
+//  * K that ends inside a stage, groups of any length: the last stage's copies are moved back to end with the row, and what of
+//    a stage does not belong to the sum is zeroed in the fragments of a.  (Where groups lie along K, in those of b and in the exponents
+//    as well: rows of other groups or of none may hold NaN.)
 //
 // Operand layout of the instruction: lane (r = lane % 16, q = lane / 16) supplies for row r the bytes K[16q, 16q + 16) in its first four
 // registers and K[64 + 16q, 64 + 16q + 16) in the last four; the 32-wide block q of row r is scaled by byte 0 of the lane's
@@ -60,8 +61,11 @@ struct WideShape {
     static constexpr int kRows = kBM + kBN;
     static constexpr int kSlot = kRows * kWideK;
     static constexpr int kPieces = kRows / 8 / 8;               // 8-row copies per wave and stage
-    static constexpr int kRing = SLOTS * kSlot;                 // [2 blocks][4 stages][rows] dwords
-    static constexpr int kTable = kRing + 8 * kRows * 4;        // tiles ahead of each group (kWideGroupRows)
+    static constexpr int kRing = SLOTS * kSlot;                 // [2 blocks][kBlock stages][rows] dwords
+    // Stages whose scales are fetched together.  Where they are taken from the registers everything that is under way is waited for, which
+    // two slots do at every stage, and more of them should not do often.
+    static constexpr int kBlock = SLOTS == 2 || NJ == 4 ? 4 : MI == 2 ? 16 : 8;
+    static constexpr int kTable = kRing + 2 * kBlock * kRows * 4;    // tiles ahead of each group (kWideGroupRows)
     static_assert(kBM % 64 == 0 && kBN % 64 == 0, "whole copies per wave, whole waves of rows");
     static_assert(MI * NJ % 4 == 0 && MI % 2 == 0, "parts and fragments take turns from stage to stage");
     static constexpr int lds_bytes(WideForm form, int groups) { return kTable + (form == kWideGroupRows ? (groups + 1) * 4 : 0); }
@@ -132,7 +136,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     using S = WideShape<MI, NJ, SLOTS>;
     constexpr int kWideBN = S::kBN;
     constexpr bool kBlocked = FORM == kWideBlock || FORM == kWideBlockRows;
-    constexpr int kBM = S::kBM, kPieces = S::kPieces;
+    constexpr bool kGroupK = FORM == kWideGroupDw;   // (what is next to a group of K in a row is not its own)
+    constexpr int kBM = S::kBM, kPieces = S::kPieces, kBlock = S::kBlock;
     const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint8_t *)wide_smem;
@@ -157,7 +162,8 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
 
     // Tile k of this workgroup, in bands of 4 tile rows; each XCD gets a contiguous range, or its part of every group
     struct Tile {
-        int64_t m0, n0, rows_end, first, end;        // rows of a below rows_end; the sum is over [first, end)
+        int64_t m0, n0, rows_end;                    // rows of a below rows_end
+        int first, end;                              // the sum is over [first, end)
         int group, T;
     };
     auto tile_of = [&](int k) {
@@ -175,7 +181,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         t.m0 = 0;
         t.rows_end = p.M;
         t.first = 0;
-        t.end = p.K;
+        t.end = (int)p.K;
         if constexpr (FORM == kWideGroupRows) {
             const GroupTiles of = group_of_tile(table, p.groups, (uint32_t)p.tiles_n, at);
             t.group = of.group;
@@ -189,23 +195,25 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
             for (uint32_t n; at >= (n = eighth_size(each, (xcd + g) & 7)); g++) at -= n;
             at += eighth_begin(each, (xcd + g) & 7);
             t.group = (int)g;
-            group_range(p.offsets, t.group, p.K, t.first, t.end);
-            t.first &= ~(int64_t)(kGroup - 1);                   // (they are multiples of 32 already, by contract)
-            t.end &= ~(int64_t)(kGroup - 1);
+            int64_t first, end;
+            group_range(p.offsets, t.group, p.K, first, end);
+            t.first = (int)first & ~(kGroup - 1);                // (they are multiples of 32 already, by contract)
+            t.end = (int)end & ~(kGroup - 1);
         }
         constexpr uint32_t kBand = 4;
         const uint32_t band = at / (kBand * (uint32_t)p.tiles_n), rem = at - band * kBand * (uint32_t)p.tiles_n;
         const uint32_t here = tiles_m - band * kBand < kBand ? tiles_m - band * kBand : kBand;
         t.n0 = (int64_t)__builtin_amdgcn_readfirstlane((int)(rem / here)) * kWideBN;
         t.m0 += (int64_t)__builtin_amdgcn_readfirstlane((int)(band * kBand + rem % here)) * kBM;
-        t.T = (int)((t.end - t.first + kWideK - 1) / kWideK);
+        t.T = (t.end - t.first + kWideK - 1) / kWideK;
         if (t.T == 0) t.T = 1;                                   // (nothing to add, but zeros to store)
         return t;
     };
     // first byte of stage P of a row: moved back where the row would end inside it
+    const int last_stage = (int)p.K - kWideK;
     auto stage_at = [&](const Tile &t, int P) {
-        const int64_t at = t.first + (int64_t)P * kWideK, last = p.K - kWideK;
-        return at < last ? at : last;
+        const int at = t.first + P * kWideK;
+        return at < last_stage ? at : last_stage;
     };
 
     // ---- what is copied
@@ -223,7 +231,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     uint32_t c_slot = 0;
     const uint8_t *sa_ptr, *sb_ptr;                  // of the stage to copy
     auto copy_begin = [&]() {
-        const int64_t at = stage_at(ct, c_P);
+        const int at = stage_at(ct, c_P);
         sa_ptr = ca + at;
         sb_ptr = cb + at;
     };
@@ -247,21 +255,21 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         }
     };
 
-    // ---- what is scaled: this thread's row, four dwords at a time
+    // ---- what is scaled: this thread's row, a block of dwords at a time
     int s_tile = 0, s_block = 0, s_blocks = 1, s_T = 1;
     const bool s_is_a = wave < kBM / kWave, s_there = wave < S::kRows / kWave && (FORM != kWideGroupRows || s_is_a);
     const uint8_t *s_base = nullptr;                 // of the tile's first row
     uint32_t s_row = 0, s_end = 0;                   // bytes from there: this row, the end of the array (no row of the tile is 4 GB away)
     uint32_t s_back = 0;                             // exponents by which the tile's last stage is moved back
-    uint32_t words[4];
-    int moved = 4;                                   // the one of them that is moved by so many exponents
+    uint32_t words[kBlock];
+    int moved = kBlock;                                   // the one of them that is moved by so many exponents
     uint32_t moved_by = 0;
     auto scale_tile = [&](const Tile &t) {
-        s_blocks = (t.T + 3) >> 2;
+        s_blocks = (t.T + kBlock - 1) / kBlock;
         s_T = t.T;
         // (from where the first stage is copied, at least four exponents ahead of the row's end)
-        const int64_t begin = stage_at(t, 0);
-        if (!kBlocked) s_back = (uint32_t)((begin + (int64_t)(t.T - 1) * kWideK - stage_at(t, t.T - 1)) >> 5);
+        const int begin = stage_at(t, 0);
+        if (!kBlocked) s_back = (uint32_t)(begin + (t.T - 1) * kWideK - stage_at(t, t.T - 1)) >> 5;
         if (!s_there) return;
         const int64_t row0 = s_is_a ? t.m0 : FORM == kWideBlock ? t.n0 >> 7 : t.n0, pitch = s_is_a ? p.pitch_a : p.pitch_b;
         const int last = (int)((s_is_a ? t.rows_end - t.m0 : p.N - t.n0) < S::kRows ? (s_is_a ? t.rows_end - t.m0 : p.N - t.n0) : S::kRows) - 1;
@@ -275,21 +283,24 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     };
     auto scale_load = [&]() {
         if (s_there) {
-            const uint32_t at = s_row + (uint32_t)s_block * 16;
-            if (at + 16 <= s_end) {
-                const u32x4_at1 v = *reinterpret_cast<const u32x4_at1 *>(s_base + at);
-                words[0] = v.x; words[1] = v.y; words[2] = v.z; words[3] = v.w;
-            } else {
-                // the array ends here: its last four bytes, moved to their place in the word
 #pragma unroll
-                for (int u = 0; u < 4; u++) {
-                    const uint32_t w = at + 4 * u, from = w + 4 <= s_end ? w : s_end - 4;
-                    words[u] = *reinterpret_cast<const u32_at1 *>(s_base + from) >> (8 * ((w - from) & 3));
+            for (int f = 0; f < kBlock / 4; f++) {
+                const uint32_t at = s_row + (uint32_t)s_block * (4 * kBlock) + 16 * f;
+                if (at + 16 <= s_end) {
+                    const u32x4_at1 v = *reinterpret_cast<const u32x4_at1 *>(s_base + at);
+                    words[4 * f] = v.x; words[4 * f + 1] = v.y; words[4 * f + 2] = v.z; words[4 * f + 3] = v.w;
+                } else {
+                    // the array ends here: its last four bytes, moved to their place in the word
+#pragma unroll
+                    for (int u = 0; u < 4; u++) {
+                        const uint32_t w = at + 4 * u, from = w + 4 <= s_end ? w : s_end - 4;
+                        words[4 * f + u] = *reinterpret_cast<const u32_at1 *>(s_base + from) >> (8 * ((w - from) & 3));
+                    }
                 }
             }
         }
         if (!kBlocked) {
-            moved = s_block == s_blocks - 1 ? (s_T - 1) & 3 : 4;
+            moved = s_block == s_blocks - 1 ? (s_T - 1) % kBlock : kBlock;
             moved_by = 8 * s_back;
         }
         if (++s_block == s_blocks) {
@@ -300,14 +311,16 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     auto scale_store = [&](int half) {
         if (s_there)
 #pragma unroll
-            for (int u = 0; u < 4; u++) ring[(half * 4 + u) * S::kRows + tid] = !kBlocked && u == moved ? words[u] << moved_by : words[u];
+            for (int u = 0; u < kBlock; u++) ring[(half * kBlock + u) * S::kRows + tid] = !kBlocked && u == moved ? words[u] << moved_by : words[u];
     };
 
     // ---- what is computed
     v4f acc[MI][NJ], part[kBlocked ? 4 : 1];
     v8i fa[2], fb[NJ];
     uint32_t sa[4] = {0, 0, 0, 0}, sb[NJ];           // exponent bytes (sb: of each fragment); scales of rows of a, of blocks of b
-    float row_scale[FORM == kWideBlockRows ? NJ : 1][4], both[2];
+    using RowScales = float[FORM == kWideBlockRows ? NJ : 1][4];
+    RowScales row_scale;
+    float both[2];
     const int sw = (r16 >> 1) & 7;
     const uint32_t lane_at = (uint32_t)(r16 * kWideK + ((q ^ sw) << 4));
     const uint32_t a_at = lane_at + (uint32_t)(wm * 16 * MI * kWideK), b_at = lane_at + (uint32_t)((kBM + wn * 16 * NJ) * kWideK);
@@ -317,38 +330,63 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
         f[0] = (int)lo.x; f[1] = (int)lo.y; f[2] = (int)lo.z; f[3] = (int)lo.w;
         f[4] = (int)hi.x; f[5] = (int)hi.y; f[6] = (int)hi.z; f[7] = (int)hi.w;
     };
-    auto read_a = [&](int i, uint32_t slot, int stage) {
-        read_fragment(fa[i & 1], a_at + slot + (uint32_t)(i * 16 * kWideK), (a_at ^ 64) + slot + (uint32_t)(i * 16 * kWideK));
+    auto a_fragment = [&](v8i &f, int i, uint32_t slot) { read_fragment(f, a_at + slot + (uint32_t)(i * 16 * kWideK), (a_at ^ 64) + slot + (uint32_t)(i * 16 * kWideK)); };
+    auto b_fragment = [&](v8i &f, int j, uint32_t slot) { read_fragment(f, b_at + slot + (uint32_t)(j * 16 * kWideK), (b_at ^ 64) + slot + (uint32_t)(j * 16 * kWideK)); };
+    auto a_scale = [&](int i, int stage) {
         const uint32_t *x = ring + stage * S::kRows + wm * 16 * MI + i * 16 + r16;
-        sa[i & 3] = kBlocked ? *x : (uint32_t)reinterpret_cast<const uint8_t *>(x)[q];
+        return kBlocked ? *x : (uint32_t)reinterpret_cast<const uint8_t *>(x)[q];
     };
-    auto read_b = [&](int j, uint32_t slot) { read_fragment(fb[j], b_at + slot + (uint32_t)(j * 16 * kWideK), (b_at ^ 64) + slot + (uint32_t)(j * 16 * kWideK)); };
-    auto read_b_scale = [&](int j, int stage) {
+    auto b_scale = [&](uint32_t (&s)[NJ], RowScales &rows, int j, int stage) {
         const uint32_t *x = ring + stage * S::kRows + kBM + wn * 16 * NJ + j * 16;
-        if (FORM == kWideBlock) {
-            if (j == 0) sb[0] = x[0];                            // (a wave's columns share it)
-        } else if (FORM == kWideBlockRows) {
+        if constexpr (FORM == kWideBlock) {
+            if (j == 0) s[0] = x[0];                             // (a wave's columns share it)
+        } else if constexpr (FORM == kWideBlockRows) {
             const float4 v = *reinterpret_cast<const float4 *>(x + 4 * q);
-            row_scale[FORM == kWideBlockRows ? j : 0][0] = v.x; row_scale[FORM == kWideBlockRows ? j : 0][1] = v.y;
-            row_scale[FORM == kWideBlockRows ? j : 0][2] = v.z; row_scale[FORM == kWideBlockRows ? j : 0][3] = v.w;
-        } else if (FORM == kWideGroupDw) {
-            sb[j] = (uint32_t)reinterpret_cast<const uint8_t *>(x + r16)[q];
+            rows[j][0] = v.x; rows[j][1] = v.y; rows[j][2] = v.z; rows[j][3] = v.w;
+        } else if constexpr (FORM == kWideGroupDw) {
+            s[j] = (uint32_t)reinterpret_cast<const uint8_t *>(x + r16)[q];
         } else {
-            sb[j] = 127;
+            s[j] = 127;
         }
+    };
+    auto read_a = [&](int i, uint32_t slot, int stage) {
+        a_fragment(fa[i & 1], i, slot);
+        sa[i & 3] = a_scale(i, stage);
     };
     // instruction number n of a stage is that of fragments (n / NJ, n % NJ); its part is n % 4
     constexpr int kAll = MI * NJ;
-    auto fold = [&](int n) {
+    auto add_part = [&](int n, uint32_t of_a, const RowScales &rows) {       // (of_a: the row's scale, or with that of the block of b)
         const int i = n / NJ, j = n % NJ;
         v4f &d = part[kBlocked ? n & 3 : 0];
         asm volatile("" : "+v"(d));
 #pragma unroll
         for (int v = 0; v < 4; v++) {
-            if (FORM == kWideBlockRows) acc[i][j][v] = __builtin_fmaf(d[v] * __uint_as_float(sa[i & 3]), row_scale[FORM == kWideBlockRows ? j : 0][v], acc[i][j][v]);
-            else acc[i][j][v] = __builtin_fmaf(d[v], both[i & 1], acc[i][j][v]);
+            if (FORM == kWideBlockRows) acc[i][j][v] = __builtin_fmaf(d[v] * __uint_as_float(of_a), rows[FORM == kWideBlockRows ? j : 0][v], acc[i][j][v]);
+            else acc[i][j][v] = __builtin_fmaf(d[v], __uint_as_float(of_a), acc[i][j][v]);
         }
         asm volatile("" : "+v"(acc[i][j]));          // (here, and not when the part's registers are needed again)
+    };
+    auto fold = [&](int n) { add_part(n, FORM == kWideBlockRows ? sa[n / NJ & 3] : __float_as_uint(both[n / NJ & 1]), row_scale); };
+
+    // Tiles with registers to spare: a wave holds all fragments and scales of its stage and reads those of the next between its matrix
+    // instructions.  The barrier is at the head of the stage: there every wave holds it, so that its slot is free, and the next has landed.
+    // (Where the fragments of a are fetched one ahead instead, a stage of 64 x 128 took 0.65 us, most of it the trip to LDS.)
+    constexpr bool kHolds = MI <= 4 && !(FORM == kWideBlockRows && NJ == 4);
+    struct Held {
+        v8i a[MI], b[NJ];
+        uint32_t sa[MI], sb[NJ];
+        RowScales rows;
+    };
+    Held held0, held1;
+    auto read_held = [&](Held &f, int x, uint32_t to) {
+        if (x < NJ) b_fragment(f.b[x], x, to);
+        else a_fragment(f.a[x - NJ], x - NJ, to);
+    };
+    auto read_held_scales = [&](Held &f, int stage) {
+#pragma unroll
+        for (int i = 0; i < MI; i++) f.sa[i] = a_scale(i, stage);
+#pragma unroll
+        for (int j = 0; j < NJ; j++) b_scale(f.sb, f.rows, j, stage);
     };
 
     // ---- the first stages
@@ -368,11 +406,17 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     wait_lds_and_barrier();
     int half = 0;
     uint32_t slot = 0;
-    read_a(0, 0, 0);
+    if constexpr (kHolds) {
 #pragma unroll
-    for (int j = 0; j < NJ; j++) {
-        read_b(j, 0);
-        read_b_scale(j, 0);
+        for (int x = 0; x < MI + NJ; x++) read_held(held0, x, 0);
+        read_held_scales(held0, 0);
+    } else {
+        read_a(0, 0, 0);
+#pragma unroll
+        for (int j = 0; j < NJ; j++) {
+            b_fragment(fb[j], j, 0);
+            b_scale(sb, row_scale, j, 0);
+        }
     }
 
     for (int k = 0; k < n_tiles; k++) {
@@ -384,31 +428,103 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
 #pragma unroll
                 for (int v = 0; v < 4; v++) acc[i][j][v] = 0.0f;
         if (kBlocked) {
-            // what the first instructions fold is nothing
+            // what the first instructions fold is nothing, whatever the scales of the tile before
             both[1] = 0.0f;
+            sa[(MI - 1) & 3] = held1.sa[MI - 1] = 0;
 #pragma unroll
             for (int j = 2; j < 4; j++)
 #pragma unroll
                 for (int v = 0; v < 4; v++) part[kBlocked ? j : 0][v] = 0.0f;
-        }
-        for (int P = 0; P < t.T; P++) {
-            const bool block_ends = (P & 3) == 3 || P == t.T - 1;
-            if ((P & 3) == 0 && s_tile < n_tiles) scale_load();
-            const int stage = half * 4 + (P & 3), next_stage = block_ends ? (half ^ 1) * 4 : stage + 1;
-            const uint32_t next_slot = slot + S::kSlot == SLOTS * S::kSlot ? 0 : slot + S::kSlot;
-            // 16-byte chunks of this stage that belong to the sum
-            const int64_t at = stage_at(t, P), from = t.first + (int64_t)P * kWideK;
-            const int64_t to = t.end < from + kWideK ? t.end : from + kWideK;
-            const int lo = (int)((from - at) >> 4), hi = (int)((to - at) >> 4);
-            const bool whole = lo == 0 && hi == 8;
-            bool copies = false;
 #pragma unroll
-            for (int i = 0; i < MI; i++) {
+            for (int j = FORM == kWideBlockRows ? NJ - 2 : 0; j < (FORM == kWideBlockRows ? NJ : 0); j++)
+#pragma unroll
+                for (int v = 0; v < 4; v++) row_scale[j][v] = held1.rows[j][v] = 0.0f;
+        }
+        // 16-byte chunks of the last stage that belong to the sum
+        const int last_from = t.first + (t.T - 1) * kWideK, last_at = stage_at(t, t.T - 1);
+        const int last_lo = (last_from - last_at) >> 4, last_hi = (t.end - last_at) >> 4;
+        const bool last_whole = last_lo == 0 && last_hi == 8;
+        // what of a fragment does not belong to the sum: zeros, and 2^0 for a block of 32
+        auto cut = [&](v8i &f) {
+#pragma unroll
+            for (int v = 0; v < 8; v++) {
+                const int c = q + (v < 4 ? 0 : 4);
+                if (c < last_lo || c >= last_hi) f[v] = 0;
+            }
+        };
+        auto cut_exponent = [&](uint32_t &e) {
+            if (2 * q < last_lo || 2 * q >= last_hi) e = 127;
+        };
+        auto one_stage = [&](int P, Held &f, Held &next) {
+            const bool block_ends = P % kBlock == kBlock - 1 || P == t.T - 1;
+            if (P % kBlock == 0 && s_tile < n_tiles) scale_load();
+            const int stage = half * kBlock + P % kBlock, next_stage = block_ends ? (half ^ 1) * kBlock : stage + 1;
+            const uint32_t next_slot = slot + S::kSlot == SLOTS * S::kSlot ? 0 : slot + S::kSlot;
+            const bool whole = P < t.T - 1 || last_whole;
+            bool copies = false;
+            if constexpr (kHolds) {
+                copies = c_tile < n_tiles;
+                if (SLOTS > 2 && copies) wait_vmcnt<(SLOTS - 2) * kPieces>();
+                else wait_vmcnt<0>();
+                if (block_ends) scale_store(half ^ 1);
+                wait_lds_and_barrier();
+                if (copies) copy_begin();
                 if (!whole) {
 #pragma unroll
-                    for (int v = 0; v < 8; v++) {
-                        const int c = q + (v < 4 ? 0 : 4);
-                        if (c < lo || c >= hi) fa[i & 1][v] = 0;
+                    for (int i = 0; i < MI; i++) {
+                        cut(f.a[i]);
+                        if (kGroupK) cut_exponent(f.sa[i]);
+                    }
+                    if (kGroupK)
+#pragma unroll
+                        for (int j = 0; j < NJ; j++) {
+                            cut(f.b[j]);
+                            cut_exponent(f.sb[j]);
+                        }
+                }
+#pragma unroll
+                for (int j = 0; j < (kGroupK ? NJ : 0); j++) asm volatile("" : "+v"(f.b[j]));
+#pragma unroll
+                for (int i = 0; i < MI; i++) {
+                    if (FORM == kWideBlock) f.sa[i] = __float_as_uint(block_scales(__uint_as_float(f.sa[i]), __uint_as_float(f.sb[0])));
+                    asm volatile("" : "+v"(f.a[i]), "+v"(f.sa[i]));
+                }
+                if (!kBlocked)
+#pragma unroll
+                    for (int j = 0; j < NJ; j++) asm volatile("" : "+v"(f.sb[j]));
+                asm volatile("s_nop 4" ::: "memory");            // vector ALU write -> operand of a matrix instruction
+#pragma unroll
+                for (int n = 0; n < kAll; n++) {
+                    const int i = n / NJ, j = n % NJ;
+                    if (kBlocked) mfma16_from_zero(part[kBlocked ? n & 3 : 0], f.b[j], f.a[i]);
+                    else mfma16_scaled(acc[i][j], f.b[j], f.a[i], f.sb[j], f.sa[i]);
+                    if (kBlocked) {
+                        // (the last two of a stage are folded in the next one, ahead of its reads of scales)
+                        if (n >= 2) add_part(n - 2, f.sa[(n + kAll - 2) % kAll / NJ], f.rows);
+                        else add_part(n + kAll - 2, next.sa[(n + kAll - 2) % kAll / NJ], next.rows);
+                    }
+#pragma unroll
+                    for (int x = n * (MI + NJ) / kAll; x < (n + 1) * (MI + NJ) / kAll; x++) read_held(next, x, next_slot);
+                    if (n == 2) read_held_scales(next, next_stage);
+                    if (copies)
+#pragma unroll
+                        for (int x = n * kPieces / kAll; x < (n + 1) * kPieces / kAll; x++) copy_piece(x);
+                    pin();
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < (kHolds ? 0 : MI); i++) {
+                if (!whole) {
+                    cut(fa[i & 1]);
+                    if (kGroupK) {
+                        cut_exponent(sa[i & 3]);
+                        if (i == 0)
+#pragma unroll
+                            for (int j = 0; j < NJ; j++) {
+                                cut(fb[j]);
+                                cut_exponent(sb[j]);
+                                asm volatile("" : "+v"(fb[j]));
+                            }
                     }
                     asm volatile("s_nop 4" : "+v"(fa[i & 1]));   // vector ALU write -> operand of a matrix instruction
                 }
@@ -429,15 +545,15 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
                         // when those of this one have been used)
                         const int n = i * NJ + j - 2, of = n >= 0 ? n : n + kAll;
                         fold(of);
-                        if (of / NJ == MI - 1 && FORM == kWideBlockRows) read_b_scale(of % NJ, n >= 0 ? next_stage : stage);
+                        if (of / NJ == MI - 1 && FORM == kWideBlockRows) b_scale(sb, row_scale, of % NJ, n >= 0 ? next_stage : stage);
                     }
                     // (with two fragments of a, the scale of the one ahead is used for the last time by this one's second fold)
                     constexpr int kReadA = FORM == kWideBlockRows && MI == 2 ? 1 : 0;
                     if (i + 1 < MI && j == kReadA) read_a(i + 1, slot, stage);
                     if (i == MI - 1) {
                         if (j == kReadA) read_a(0, next_slot, next_stage);
-                        read_b(j, next_slot);
-                        if (FORM != kWideBlockRows) read_b_scale(j, next_stage);
+                        b_fragment(fb[j], j, next_slot);
+                        if (FORM != kWideBlockRows) b_scale(sb, row_scale, j, next_stage);
                         if (copies)
 #pragma unroll
                             for (int x = j * kPieces / NJ; x < (j + 1) * kPieces / NJ; x++) copy_piece(x);
@@ -457,13 +573,28 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
             if (copies) copy_end();
             if (block_ends) half ^= 1;
             slot = next_slot;
+        };
+        if constexpr (kHolds) {
+            for (int P = 0; P < t.T; P += 2) {
+                one_stage(P, held0, held1);
+                if (P + 1 < t.T) one_stage(P + 1, held1, held0);
+            }
+        } else {
+            for (int P = 0; P < t.T; P++) one_stage(P, held0, held0);
         }
         // ---- epilogue: straight from the registers
         float scale = 1.0f;
         if (kBlocked) {
             asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");   // the last matrix instructions retire
-            fold(kAll - 2);
-            fold(kAll - 1);
+#pragma unroll
+            for (int n = kAll - 2; n < kAll; n++) {
+                if constexpr (kHolds) {
+                    if (t.T & 1) add_part(n, held0.sa[n / NJ], held0.rows);
+                    else add_part(n, held1.sa[n / NJ], held1.rows);
+                } else {
+                    fold(n);
+                }
+            }
         } else {
             scale = *p.a_s * p.b_s[FORM == kWideGroupRows ? t.group * p.b_s_stride : 0];
             asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
@@ -472,6 +603,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
 #pragma unroll
                 for (int j = 0; j < NJ; j++) asm volatile("" : "+v"(acc[i][j]));
         }
+        if (kHolds && (t.T & 1)) held0 = held1;                  // (the next tile's first stage)
         void *out = p.out;
         if (FORM == kWideGroupDw) out = (uint8_t *)p.out + (int64_t)t.group * p.M * p.ld_out * (p.out_f32 ? 4 : 2);
 #pragma unroll

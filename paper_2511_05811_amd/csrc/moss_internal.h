@@ -61,6 +61,25 @@ int moss_internal_gemm_mid(int kind, int64_t M, int64_t N, int64_t K, const uint
                            const uint8_t *b_q, const uint8_t *b_e, const float *b_s, void *out, int out_f32, int64_t ld_out,
                            int accumulate, hipStream_t st);
 
+// Time of a product in one kind of tiles, in microseconds, by which a kind is chosen: a launch, then for each round of tiles over the
+// compute units a fixed part and one per stage, and a part for every tile (what its rows and outputs cost the memory).
+// A persistent grid (`persistent`) waits for its last, half full round; otherwise `at_a_time` workgroups run on a compute unit.
+struct MossTileCost {
+    double launch, round, stage, tile, ragged;       // (ragged: K that ends inside a stage, or unaligned rows, per stage)
+    int bm, bn, k_groups, at_a_time;
+    bool persistent;
+};
+static inline double moss_tile_us(const MossTileCost &c, double tiles, double stages, bool ragged)
+{
+    int cus = moss_internal_cu_count();
+    if (cus <= 0) cus = 256;
+    const double u = tiles / cus;
+    double rounds = c.persistent ? (u > 1.0 ? u + 0.5 : 1.0) : u / c.at_a_time;
+    if (rounds < 1.0) rounds = 1.0;
+    return c.launch + rounds * (c.round + stages * c.stage * (ragged ? 1.0 + c.ragged : 1.0)) + u * c.tile;
+}
+static inline int64_t moss_ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
 namespace moss {
 
 constexpr int kWave = 64;
