@@ -333,8 +333,9 @@ int moss_quant_block128_weight(const void *w, int w_dtype, int64_t rows, int64_t
  * The three products of a linear layer:
  *   Y = X W^T: (Xq_row, s_row), (Wq, s), 128;  dX = dY W: (dYq_row, s_row), (Wq_t, s_t), 128;
  *   dW = dY^T X: (dYq_col, s_col), (Xq_col, s_col), 1.
- * The product of two scales is capped at FLT_MAX.  A block's products are summed by the matrix unit, the blocks in FP32 in order of K (K split in up to four parts, each in order,
- * where the problem is small: the choice goes by sizes alone).
+ * A block's products are summed by the matrix unit, the blocks in FP32 in order of K (K split in up to four parts, each in order,
+ * where the problem is small: the choice goes by sizes alone).  A block whose codes are all zeros adds nothing, whatever its finite
+ * scales are; otherwise the product of two scales has to be finite, and with b_block 1 a block's sum times a_s as well.
  * Requirements: K % 32 == 0, K <= 2^22; ld_out >= N; 16-byte aligned codes and out. */
 int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, const float *a_s, const uint8_t *b_q, const float *b_s,
                            int64_t b_block, void *out, int out_dtype, int64_t ld_out, int accumulate, void *stream);
@@ -358,7 +359,9 @@ int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, 
  *   a_q [M x rows], a_e [M x rows/32], b_q [N x rows], b_e [N x rows/32]: column groupings of the two-level quantizer.
  *   out  [groups x M x N] dense; a group without rows gets zeros (or, accumulating, stays as it is).
  *   Requirements: rows % 32 == 0, rows <= 2^24, offsets that are multiples of 32.
- * Both: groups <= 1024, BF16 or FP32 outputs, accumulate only with FP32; otherwise as moss_gemm_fp8_mx.
+ *   What rows of other groups or of none hold, NaN codes and exponents among it, makes no difference.
+ * Both: groups <= 1024; ceil(rows/128) groups ceil(N/128) < 2^27 (_dw: groups ceil(M/128) ceil(N/128)); BF16 or FP32 outputs,
+ * accumulate only with FP32; otherwise as moss_gemm_fp8_mx.
  * ------------------------------------------------------------------------- */
 int moss_gemm_fp8_mx_grouped(int64_t rows, int64_t N, int64_t K, int64_t groups, const int32_t *offsets, const uint8_t *a_q,
                              const uint8_t *a_e, const float *a_s, const uint8_t *b_q, int64_t ld_b, int64_t b_stride,
@@ -390,7 +393,8 @@ int moss_gemm_fp8_mx_grouped_dw(int64_t rows, int64_t M, int64_t N, int64_t grou
  *
  * x, out, d_out: BF16 [tokens x cols]; y, d_y: BF16 [rows x cols]; weights, d_weights: FP32 [tokens x k] dense.
  * Requirements: cols % 8 == 0, row strides >= cols and multiples of 8, finite inputs.  Entries of row_of and source outside their
- * ranges count as -1; a row_of with one row twice, or a source that does not belong to it, leaves unspecified values.      */
+ * ranges count as -1; a row_of with one row twice, or a source that does not belong to it, leaves unspecified values.
+ * Outputs overlap no input, except that d_y may be y.      */
 int64_t moss_expert_rows(int64_t tokens, int64_t k, int64_t n_experts, int64_t multiple);
 int moss_expert_plan(const int32_t *experts, int64_t tokens, int64_t k, int64_t n_experts, int64_t multiple, int64_t rows,
                      int32_t *row_of, int32_t *source, int32_t *offsets, void *stream);

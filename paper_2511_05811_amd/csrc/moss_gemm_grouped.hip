@@ -82,8 +82,8 @@ template <moss::MidForm FORM>
 int launch_small(int kind, const moss::MidGroupArgs &p, hipStream_t st)
 {
     if constexpr (FORM == moss::kMidGroupRows) {
-        if (kind == kSmall32) return moss::launch_mid_kind<FORM, 0>(p, st);
-        if (kind == kSmall64) return moss::launch_mid_kind<FORM, 2>(p, st);
+        const int rc = kind == kSmall32 ? moss::launch_mid_kind<FORM, 0>(p, st) : kind == kSmall64 ? moss::launch_mid_kind<FORM, 2>(p, st) : MOSS_ERR_UNSUPPORTED;
+        if (rc != MOSS_ERR_UNSUPPORTED) return rc;           // (there may be too many of them)
     }
     return moss::launch_mid_kind<FORM, 3>(p, st);
 }
