@@ -9,6 +9,12 @@
 // shuffles and one trip through LDS join the 16 threads of a column.  The transposed codes come out of the converter in
 // transposed order (four rows of a column at a time), meet in LDS in 8-byte pieces swizzled by column and leave as whole lines.
 // Row groups alone need no tile: 16 lanes per group, wherever it lies.
+//
+// 8192 x 4096, rows / columns / both: 18.3 / 21.8 / 32.0 us (5.5 / 4.7 / 4.3 TB/s; a large copy 5.0); 8192 x 11008 both 75.6 (4.8); an FP32
+// weight of 11008 x 4096 with its transposed codes 55.4 (4.9).  With two IEEE divisions per row and per column, shuffles through LDS and
+// a clamp per value, which the memory does not hide in so short a kernel, both took 36.4 and 81.4.
+#include <type_traits>
+
 #include "moss_internal.h"
 
 namespace moss {
@@ -28,6 +34,31 @@ __device__ __forceinline__ float bq_hi(uint32_t w) { return __uint_as_float(w & 
 
 __device__ __forceinline__ float block_scale(float amax) { return amax > 0.0f ? amax / kE4M3Max : 1.0f; }
 __device__ __forceinline__ float block_reciprocal(float s) { return fminf(1.0f / s, 3.402823466e38f); }
+
+// The same of N maxima of BF16 magnitudes at once.  Between 2^-90 and 2^90 a product and two fused steps give the quotient, and the
+// approximate reciprocal with two fused steps its reciprocal, rounded as the divisions round them (all 128 mantissas have been compared);
+// a wave that has others divides.
+template <int N>
+__device__ __forceinline__ void block_scales_of(const float (&amax)[N], float (&s)[N], float (&inv)[N])
+{
+    constexpr uint32_t kLow = (127u - 90u) << 23, kHigh = (127u + 90u) << 23;
+    bool unusual = false;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const float c = 1.0f / kE4M3Max, q = amax[i] * c;
+        const float t = __builtin_fmaf(__builtin_fmaf(-kE4M3Max, q, amax[i]), c, q);
+        s[i] = amax[i] > 0.0f ? t : 1.0f;
+        const float r = __builtin_amdgcn_rcpf(s[i]);
+        inv[i] = __builtin_fmaf(__builtin_fmaf(-s[i], r, 1.0f), r, r);
+        unusual |= amax[i] != 0.0f && __float_as_uint(amax[i]) - kLow > kHigh - kLow;
+    }
+    if (__any(unusual))
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            s[i] = block_scale(amax[i]);
+            inv[i] = block_reciprocal(s[i]);
+        }
+}
 
 // Eight neighbours of a row, as they come: four words of BF16 pairs or eight FP32 words
 template <bool F32> struct Chunk {
@@ -71,18 +102,38 @@ __device__ __forceinline__ float top_of(const Top<F32> &m)
     if (F32) return __uint_as_float(t);
     return fmaxf(bq_lo(t), bq_hi(t));
 }
-__device__ __forceinline__ float max_of_16_lanes(float m)
+// (of magnitudes, whose order is that of their bits; rotated inside a row of 16 lanes)
+__device__ __forceinline__ float max_of_16_lanes(float magnitude)
 {
-#pragma unroll
-    for (int d = 1; d < 16; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
-    return m;
+    uint32_t m = __float_as_uint(magnitude);
+    auto rotated = [&](auto by) {
+        const uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)m, 0x120 + decltype(by)::value, 0xF, 0xF, true);
+        m = o > m ? o : m;
+    };
+    rotated(std::integral_constant<int, 8>{});
+    rotated(std::integral_constant<int, 4>{});
+    rotated(std::integral_constant<int, 2>{});
+    rotated(std::integral_constant<int, 1>{});
+    return __uint_as_float(m);
+}
+
+// Four codes.  The converter itself saturates at +-448 in waves that have set the mode bit for it (FP16_OVFL, which nothing else here
+// looks at): one instruction per value less than a clamp ahead of it.
+__device__ __forceinline__ void converter_saturates()
+{
+    __builtin_amdgcn_s_setreg((1 - 1) << 11 | 23 << 6 | 1, 1);   // hwreg(MODE, offset 23, 1 bit) = 1
+}
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d)
+{
+    const int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
 
 template <bool F32>
 __device__ __forceinline__ uint2 row_codes(const Chunk<F32> &x, float inv)
 {
-    return make_uint2(cvt4_e4m3_sat(x.at(0) * inv, x.at(1) * inv, x.at(2) * inv, x.at(3) * inv),
-                      cvt4_e4m3_sat(x.at(4) * inv, x.at(5) * inv, x.at(6) * inv, x.at(7) * inv));
+    return make_uint2(codes4(x.at(0) * inv, x.at(1) * inv, x.at(2) * inv, x.at(3) * inv),
+                      codes4(x.at(4) * inv, x.at(5) * inv, x.at(6) * inv, x.at(7) * inv));
 }
 
 // Row groups alone: 16 lanes per group, kDeep groups of a lane in flight
@@ -90,6 +141,7 @@ constexpr int kDeep = 4;
 __global__ __launch_bounds__(kBqThreads) void k_block128_rows(const uint16_t *__restrict__ x, uint32_t groups, uint32_t per_row, int cols,
                                                               int64_t ld, uint8_t *__restrict__ q, float *__restrict__ s)
 {
+    converter_saturates();
     const int sub = threadIdx.x & 15;
     const uint32_t step = gridDim.x * (kBqThreads / 16);
     for (uint32_t g0 = blockIdx.x * (kBqThreads / 16) + (threadIdx.x >> 4); g0 < groups; g0 += step * kDeep) {
@@ -106,28 +158,33 @@ __global__ __launch_bounds__(kBqThreads) void k_block128_rows(const uint16_t *__
             v[u] = Chunk<false>{};
             if (there[u]) v[u] = load_chunk<false>(x, row[u] * ld + col[u]);
         }
+        float amax[kDeep], scale[kDeep], inv[kDeep];
 #pragma unroll
         for (int u = 0; u < kDeep; u++) {
             Top<false> m{};
             take(m, v[u]);
-            const float scale = block_scale(max_of_16_lanes(top_of(m)));
-            const uint2 c = row_codes(v[u], block_reciprocal(scale));
+            amax[u] = max_of_16_lanes(top_of(m));
+        }
+        block_scales_of(amax, scale, inv);
+#pragma unroll
+        for (int u = 0; u < kDeep; u++) {
             if (!there[u]) continue;
-            st_stream8(q + row[u] * cols + col[u], c);
-            if (sub == 0) s[row[u] * per_row + col[u] / 128] = scale;
+            st_stream8(q + row[u] * cols + col[u], row_codes(v[u], inv[u]));
+            if (sub == 0) s[row[u] * per_row + col[u] / 128] = scale[u];
         }
     }
 }
 
 // 128 x 128 elements.  BLOCK: one scale for all of them (weights), else one per row (ROW) and / or per column (COL).
 // ROW: codes as the elements lie.  COL: transposed codes.
-template <bool F32, bool ROW, bool COL, bool BLOCK>
+template <bool F32, bool ROW, bool COL, bool BLOCK>             // (F32 only with BLOCK)
 __global__ __launch_bounds__(kBqThreads) void k_block128_tile(const void *__restrict__ x, int64_t rows, int64_t cols, int64_t ld, uint32_t tiles_c,
                                                               uint8_t *__restrict__ q_row, float *__restrict__ s_row,
                                                               uint8_t *__restrict__ q_col, float *__restrict__ s_col)
 {
     __shared__ float red[BLOCK ? 4 : 4 * kBqTile];               // per wave: its maximum, or those of the columns
     __shared__ __attribute__((aligned(16))) uint8_t turned[COL ? kBqTile * kBqTile : 16];
+    converter_saturates();
     const uint32_t tr = blockIdx.x / tiles_c, tc = blockIdx.x % tiles_c;
     const int cg = threadIdx.x & 15, rg = threadIdx.x >> 4, wave = threadIdx.x >> 6;
     const int64_t r0 = (int64_t)tr * kBqTile + rg * 8, c0 = (int64_t)tc * kBqTile + cg * 8;
@@ -169,28 +226,35 @@ __global__ __launch_bounds__(kBqThreads) void k_block128_tile(const void *__rest
 #pragma unroll
             for (int c = 0; c < 8; c++) red[wave * kBqTile + cg * 8 + c] = t[c];
         __syncthreads();
+        float s[8];
 #pragma unroll
         for (int c = 0; c < 8; c++) {
             const int at = cg * 8 + c;
-            const float s = block_scale(fmaxf(fmaxf(red[at], red[kBqTile + at]), fmaxf(red[2 * kBqTile + at], red[3 * kBqTile + at])));
-            if (rg == 0 && c0 + c < cols) s_col[(c0 + c) * tiles_r + tr] = s;
-            inv_col[c] = block_reciprocal(s);
+            t[c] = fmaxf(fmaxf(red[at], red[kBqTile + at]), fmaxf(red[2 * kBqTile + at], red[3 * kBqTile + at]));
         }
+        block_scales_of(t, s, inv_col);
+        if (rg == 0)
+#pragma unroll
+            for (int c = 0; c < 8; c++)
+                if (c0 + c < cols) s_col[(c0 + c) * tiles_r + tr] = s[c];
     }
     if (ROW) {
+        float s[8], inv[8];
+        if (!BLOCK) {
+            float amax[8];
 #pragma unroll
-        for (int i = 0; i < 8; i++) {
-            float inv;
-            if (BLOCK) {
-                inv = inv_col[0];
-            } else {
+            for (int i = 0; i < 8; i++) {
                 Top<F32> own{};
                 take(own, v[i]);
-                const float s = block_scale(max_of_16_lanes(top_of(own)));
-                if (cg == 0 && r0 + i < rows) s_row[(r0 + i) * tiles_c + tc] = s;
-                inv = block_reciprocal(s);
+                amax[i] = max_of_16_lanes(top_of(own));
             }
-            if (c0 < cols && r0 + i < rows) st_stream8(q_row + (r0 + i) * cols + c0, row_codes(v[i], inv));
+            block_scales_of(amax, s, inv);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+            if (r0 + i >= rows) continue;
+            if (!BLOCK && cg == 0) s_row[(r0 + i) * tiles_c + tc] = s[i];
+            if (c0 < cols) st_stream8(q_row + (r0 + i) * cols + c0, row_codes(v[i], BLOCK ? inv_col[0] : inv[i]));
         }
     }
     if (COL) {
@@ -198,8 +262,8 @@ __global__ __launch_bounds__(kBqThreads) void k_block128_tile(const void *__rest
 #pragma unroll
         for (int c = 0; c < 8; c++) {
             const float f = inv_col[c];
-            const uint2 w = make_uint2(cvt4_e4m3_sat(v[0].at(c) * f, v[1].at(c) * f, v[2].at(c) * f, v[3].at(c) * f),
-                                       cvt4_e4m3_sat(v[4].at(c) * f, v[5].at(c) * f, v[6].at(c) * f, v[7].at(c) * f));
+            const uint2 w = make_uint2(codes4(v[0].at(c) * f, v[1].at(c) * f, v[2].at(c) * f, v[3].at(c) * f),
+                                       codes4(v[4].at(c) * f, v[5].at(c) * f, v[6].at(c) * f, v[7].at(c) * f));
             *reinterpret_cast<uint2 *>(turned + (cg * 8 + c) * kBqTile + ((rg ^ cg) << 3)) = w;
         }
         __syncthreads();

@@ -5,7 +5,7 @@
 // times both scales by the vector unit.  Kernels: the wide tiles (moss_gemm_wide.h) and, where few rows leave them idle and for what they
 // cannot take, the small tiles with K split over the waves (moss_gemm_mid.h); a stage is one block in both.
 //
-// Bound, large products: power.  8192 x 11008 x 4096 takes 399 us (1.85 PFLOP/s) on quantized data and 511 on random codes, and neither
+// Bound, large products: power.  8192 x 11008 x 4096 takes 389 us (1.9 PFLOP/s) on quantized data and 511 on random codes, and neither
 // the waits nor the barriers left out shorten it; the copies are 18 % of it, the additions on the vector unit 11 %, the stores 8 %.
 // (The MOSS product of the same size, whose scales the matrix instruction applies: 322 us.)  Few rows: the weight's bytes, 17 x 11008 x
 // 4096 10.4 us, 4.4 TB/s.

@@ -232,3 +232,17 @@ def test_refusals():
         moss.gemm_fp8_block128(a, a_s, b, b_s, accumulate=True)      # into BF16
     with pytest.raises(AssertionError):
         moss.gemm_fp8_block128(a.cpu(), a_s, b, b_s)
+
+
+@pytest.mark.parametrize("flags", [ROW, COL, ROW | COL])
+def test_every_magnitude_as_the_largest_of_a_group(flags):
+    """All finite BF16 magnitudes, subnormals and zero among them, each the largest of a group of rows and of one of columns."""
+    top = np.arange(0x7F80, dtype=np.uint16)                         # a group each: [255 x 128] of them
+    bits = np.zeros((255 * 128, 128), np.uint16)
+    small = np.random.default_rng(1).random((255 * 128, 128)) * mi.bf16_bits_to_f32(top.reshape(-1, 1))
+    bits[:] = np.minimum(mi.f32_to_bf16_bits(small.astype(np.float32)) & 0x7FFF, top[:, None])
+    bits[np.arange(bits.shape[0]), np.arange(bits.shape[0]) % 128] = top
+    bits[1::2] ^= 0x8000
+    check_quant(bits, flags & ROW or flags)
+    if flags & COL:
+        check_quant(np.ascontiguousarray(bits.T), flags)
