@@ -6,6 +6,10 @@
 // multiplied (gradient of combine); rows of zeros between the experts' rows are items of their own behind the tokens.  16 bytes
 // per thread, half a wave or a wave per token.  Sums and products in FP32, one rounding to BF16 at the end.  The tensors
 // that a quantizer reads leave their maximum behind, as the other BF16 producers do.
+//
+// 8192 tokens of 4096 columns, two of 64 experts each: plan 9.0 us, dispatch 38.5, combine 37.2, its gradient 74.3, that of dispatch
+// 36.6 (4.3 TB/s over all of them, a large copy 5.0; four chunks of a row under way per thread, two or eight are slower).  64 tokens of
+// 256: 3 to 5 us each, a launch and two or three trips to memory behind one another.
 #include "moss_internal.h"
 #include "moss_producer.h"
 

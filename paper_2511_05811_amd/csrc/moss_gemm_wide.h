@@ -7,7 +7,8 @@
 //  * Stages go through SLOTS slots of LDS, filled by direct global->LDS copies of 128 bytes per row.  One barrier per stage, behind the
 //    last fragment's reads of a: there the stage's slot is free, for the copies of stage + SLOTS, and the next stage has landed.  Its first fragments
 //    are read behind the last matrix instructions of this one, each b fragment behind the instruction that used its registers
-//    last.  While one wave waits its neighbour on the SIMD computes.
+//    last.  While one wave waits its neighbour on the SIMD computes.  Tiles of up to 128 rows have the registers to hold a whole stage,
+//    and with them all its reads stand ahead of the barrier (kHolds).
 //  * Blocked forms: an instruction starts from zero and leaves its sum in one of four parts.  A part is added to the accumulators
 //    times its scales when two further instructions have been issued; the matrix unit takes them one after the other, so it has
 //    retired by then.  This order is all that protects the read; the instructions are volatile asm and a part passes through an
@@ -20,6 +21,11 @@
 //  * K that ends inside a stage, groups of any length: the last stage's copies are moved back to end with the row, and what of
 //    a stage does not belong to the sum is zeroed in the fragments of a.  (Where groups lie along K, in those of b and in the exponents
 //    as well: rows of other groups or of none may hold NaN.)
+//
+// A stage takes (us; blocks of 128 of a weight / of rows / dW of groups) 1.56 / 1.90 / 2.3 to 2.7 in 256 x 256 tiles, 0.95 / 1.19 / 1.2 to
+// 1.4 in 128 x 256, 0.67 / 0.79 in 128 x 128, 0.53 / 0.57 in 64 x 128; the matrix instructions of 256 x 256 alone 1.05.  Bound: power and
+// the vector unit's sums in the blocked forms (matrix unit busy 48 % of the time, no LDS conflicts); the copies for dW, whose rows begin
+// anywhere in a line; LDS reads in the smallest tiles.
 //
 // Operand layout of the instruction: lane (r = lane % 16, q = lane / 16) supplies for row r the bytes K[16q, 16q + 16) in its first four
 // registers and K[64 + 16q, 64 + 16q + 16) in the last four; the 32-wide block q of row r is scaled by byte 0 of the lane's
@@ -547,11 +553,9 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
                         fold(of);
                         if (of / NJ == MI - 1 && FORM == kWideBlockRows) b_scale(sb, row_scale, of % NJ, n >= 0 ? next_stage : stage);
                     }
-                    // (with two fragments of a, the scale of the one ahead is used for the last time by this one's second fold)
-                    constexpr int kReadA = FORM == kWideBlockRows && MI == 2 ? 1 : 0;
-                    if (i + 1 < MI && j == kReadA) read_a(i + 1, slot, stage);
+                    if (i + 1 < MI && j == 0) read_a(i + 1, slot, stage);
                     if (i == MI - 1) {
-                        if (j == kReadA) read_a(0, next_slot, next_stage);
+                        if (j == 0) read_a(0, next_slot, next_stage);
                         b_fragment(fb[j], j, next_slot);
                         if (FORM != kWideBlockRows) b_scale(sb, row_scale, j, next_stage);
                         if (copies)
