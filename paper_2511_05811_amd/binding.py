@@ -111,7 +111,8 @@ def _bind_calls():
     names = ("moss_quant_workspace_bytes", "moss_quant_act_2level", "moss_quant_act_2level_given_max", "moss_gemm_fp8_mx",
              "moss_weight_workspace_bytes", "moss_weight_autoscale_cast", "moss_internal_swiglu_bf16", "moss_internal_swiglu_bf16_backward",
              "moss_internal_add_rmsnorm_bf16", "moss_internal_rmsnorm_bf16_backward",     # (these take scratch)
-             "moss_quant_block128", "moss_gemm_fp8_block128", "moss_gemm_fp8_mx_grouped", "moss_gemm_fp8_mx_grouped_dw", "moss_expert_rows",
+             "moss_quant_block128", "moss_quant_block128_weight", "moss_gemm_fp8_block128", "moss_gemm_fp8_mx_grouped",
+             "moss_gemm_fp8_mx_grouped_dw", "moss_expert_rows",
              "moss_expert_plan", "moss_internal_expert_dispatch_bf16", "moss_expert_combine_bf16", "moss_internal_expert_combine_bf16_backward")
     try:
         from . import _moss_calls as native
@@ -507,6 +508,11 @@ def quant_block128(x, flags=MOSS_Q_ROW, out=None):
 def quant_block128_weight(w, want_transpose=False, wq=None, s=None, wq_t=None, s_t=None):
     """(wq, s, wq_t, s_t) of a dense float32 or bfloat16 weight [rows, cols] in blocks of 128 x 128; the transposed two are None
     unless asked for (or given)."""
+    native = _bind_calls() if _calls is None else _calls
+    if native:
+        done = native.quant_block128_weight(w, want_transpose, wq, s, wq_t, s_t)
+        if done is not None:
+            return done
     import torch
     L = load()
     assert w.dim() == 2 and w.is_contiguous()

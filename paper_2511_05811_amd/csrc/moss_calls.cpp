@@ -32,6 +32,7 @@ struct Library {
     decltype(&moss_internal_add_rmsnorm_bf16) add_rmsnorm_bf16;
     decltype(&moss_internal_rmsnorm_bf16_backward) rmsnorm_bf16_backward;
     decltype(&moss_quant_block128) quant_block128;
+    decltype(&moss_quant_block128_weight) quant_block128_weight;
     decltype(&moss_gemm_fp8_block128) gemm_fp8_block128;
     decltype(&moss_gemm_fp8_mx_grouped) gemm_fp8_mx_grouped;
     decltype(&moss_gemm_fp8_mx_grouped_dw) gemm_fp8_mx_grouped_dw;
@@ -569,6 +570,42 @@ PyObject *quant_block128(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// the caller's dense tensor of that type and shape, or a new one
+bool dense_or_new(PyObject *given, Output &o, at::ScalarType type, at::IntArrayRef shape, const at::Tensor &like)
+{
+    const at::Tensor *t;
+    if (!optional(given, t) || (t && !dense(t, type, shape))) return false;
+    if (t) o.take(given, t);
+    else o.set(make(shape, type, like));
+    return true;
+}
+
+// (w, want_transpose, wq, s, wq_t, s_t)
+PyObject *quant_block128_weight(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *w;
+        PLAIN_OR_NONE(n == 6 && plain_state() && (w = plain(a[0])) && w->dim() == 2 && w->is_contiguous() && PyBool_Check(a[1]));
+        const int type = dtype_of(*w);
+        PLAIN_OR_NONE(type >= 0);
+        const int64_t rows = w->size(0), cols = w->size(1), r = (rows + 127) / 128, c = (cols + 127) / 128;
+        Output q, s, q_t, s_t;
+        PLAIN_OR_NONE(dense_or_new(a[2], q, at::kByte, {rows, cols}, *w) && dense_or_new(a[3], s, at::kFloat, {r, c}, *w));
+        if (a[1] == Py_True || a[4] != Py_None)
+            PLAIN_OR_NONE(dense_or_new(a[4], q_t, at::kByte, {cols, rows}, *w) && dense_or_new(a[5], s_t, at::kFloat, {c, r}, *w));
+        long device;
+        void *stream;
+        if (!current_place(device, stream)) return nullptr;
+        PLAIN_OR_NONE(all_on(device, {w, &q.t, &s.t}) && (!q_t.o || all_on(device, {&q_t.t, &s_t.t})));
+        void *pw = ptr(w);
+        uint8_t *pq = bytes(&q.t), *pqt = q_t.o ? bytes(&q_t.t) : nullptr;
+        float *ps = (float *)ptr(&s.t), *pst = q_t.o ? (float *)ptr(&s_t.t) : nullptr;
+        const int rc = without_gil([&] { return lib.quant_block128_weight(pw, type, rows, cols, pq, ps, pqt, pst, stream); });
+        if (!checked(rc, "moss_quant_block128_weight")) return nullptr;
+        return PyTuple_Pack(4, q.o, s.o, q_t.o ? q_t.o : Py_None, q_t.o ? s_t.o : Py_None);
+    });
+}
+
 // (a_q, a_s, b_q, b_s, out, accumulate); without `out` the result is BF16
 PyObject *gemm_fp8_block128(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
@@ -837,7 +874,8 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 
 #define CALL(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {CALL(bind), CALL(quant_act_2level), CALL(quant_act_2level_given_max), CALL(gemm_fp8_mx), CALL(weight_autoscale_cast),
-                         CALL(swiglu_bf16), CALL(swiglu_bf16_backward), CALL(add_rmsnorm_bf16), CALL(rmsnorm_bf16_backward), CALL(quant_block128), CALL(gemm_fp8_block128),
+                         CALL(swiglu_bf16), CALL(swiglu_bf16_backward), CALL(add_rmsnorm_bf16), CALL(rmsnorm_bf16_backward), CALL(quant_block128),
+                         CALL(quant_block128_weight), CALL(gemm_fp8_block128),
                          CALL(gemm_fp8_mx_grouped), CALL(gemm_fp8_mx_grouped_dw), CALL(expert_plan), CALL(expert_dispatch_bf16),
                          CALL(expert_combine_bf16), CALL(expert_combine_bf16_backward),
                          {nullptr, nullptr, 0, nullptr}};

@@ -3,7 +3,7 @@
 //      out[m, n] (+)= sum_kb a_s[m, kb] b_s[n or n / 128, kb] sum_{k in kb} dec(a[m, k]) dec(b[n, k]).
 // The scales cannot leave the main loop: the sum of every block is taken from zero by the matrix unit and added to the accumulators
 // times both scales by the vector unit.  Kernels: the wide tiles (moss_gemm_wide.h) and, where few rows leave them idle and for what they
-// cannot take, the small tiles with K split over the waves (moss_gemm_mid.h); a stage is one block in both.
+// cannot take, the small tiles (moss_gemm_mid.h); a stage is one block in both.
 //
 // Bound, large products: power.  8192 x 11008 x 4096 takes 389 us (1.9 PFLOP/s) on quantized data and 511 on random codes, and neither
 // the waits nor the barriers left out shorten it; the copies are 18 % of it, the additions on the vector unit 11 %, the stores 8 %.
@@ -14,7 +14,7 @@
 
 namespace {
 
-enum BlockKind { kBlockSmall, kBlock64, kBlock128, kBlockHalf, kBlockWide };
+enum BlockKind { kBlockSmall, kBlock64, kBlock128, kBlockHalf, kBlockWide, kBlockSmall64 };
 
 // Fits to 400 random products (M 1 to 16384, N 256 to 11008, K 32 to 8192; a scale per 128 rows of b, or per row), each run in every
 // kind of tiles: the kind chosen took 0.5 % (1.0 %) more than the fastest of its problem.  us, a scale per
@@ -35,14 +35,23 @@ constexpr MossTileCost kCost[2][5] = {{{2.2, 0.73, 0.52, 0.89, 0.12, 32, 32, 4, 
                                        {4.3, 1.14, 1.19, 3.26, 0.03, 128, 256, 1, 1, true},
                                        {7.3, 0.0, 1.9, 6.9, 0.04, 256, 256, 1, 1, true}}};
 
+// What the wide tiles cannot take (K below a stage, pieces of 16 bytes that end inside a row of the output) goes to small tiles of 32 x 32, K
+// split over their waves, or of 64 x 64.  us: 512 x 1001 x 1024 5.5 / 8.6, 1152 x 3968 x 32 27.6 / 12.0, 8192 x 4096 x 64 175 / 56,
+// 2048 x 1001 x 4096 33.2 / 25.1, 4096 x 4100 x 1024 122 / 60.
+constexpr MossTileCost kCostSmall64 = {4.0, 0.8, 0.31, 0.3, 0.0, 64, 64, 1, 1, false};
+
+double tiles_us(const MossTileCost &c, int64_t M, int64_t N, int64_t K)
+{
+    return moss_tile_us(c, (double)moss_ceil_div(M, c.bm) * (double)moss_ceil_div(N, c.bn), (double)moss_ceil_div(K, 128 * c.k_groups), K % 128 != 0);
+}
+
 int block_kind(int64_t M, int64_t N, int64_t K, int64_t b_block, int64_t ld_out)
 {
-    if (K < 128 || N % 8 || ld_out % 8) return kBlockSmall;       // (what the wide tiles cannot take)
+    if (K < 128 || N % 8 || ld_out % 8) return tiles_us(kCostSmall64, M, N, K) < tiles_us(kCost[0][kBlockSmall], M, N, K) ? kBlockSmall64 : kBlockSmall;
     int best = 0;
     double least = 0.0;
     for (int k = 0; k < 5; k++) {
-        const MossTileCost &c = kCost[b_block == 1][k];
-        const double us = moss_tile_us(c, (double)moss_ceil_div(M, c.bm) * (double)moss_ceil_div(N, c.bn), (double)moss_ceil_div(K, 128 * c.k_groups), K % 128 != 0);
+        const double us = tiles_us(kCost[b_block == 1][k], M, N, K);
         if (k == 0 || us < least) {
             best = k;
             least = us;
@@ -67,7 +76,8 @@ int launch_block(int kind, const moss::WideArgs &p, hipStream_t st)
 // The tile (rows * 1000 + columns) that a product takes (the tests hold the choice by it)
 extern "C" int moss_internal_gemm_block_tile(int64_t M, int64_t N, int64_t K, int64_t b_block, int64_t ld_out)
 {
-    const MossTileCost &c = kCost[0][block_kind(M, N, K, b_block, ld_out)];
+    const int k = block_kind(M, N, K, b_block, ld_out);
+    const MossTileCost &c = k == kBlockSmall64 ? kCostSmall64 : kCost[0][k];
     return c.bm * 1000 + c.bn;
 }
 
@@ -85,7 +95,7 @@ extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uin
     hipStream_t st = (hipStream_t)stream;
     const int64_t blocks = (K + 127) / 128;
     const int kind = block_kind(M, N, K, b_block, ld_out);
-    if (kind != kBlockSmall) {
+    if (kind != kBlockSmall && kind != kBlockSmall64) {
         WideArgs p{};
         p.M = M; p.N = N; p.K = K;
         p.a_q = a_q; p.b_q = b_q;
@@ -104,5 +114,6 @@ extern "C" int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uin
     p.b_q = b_q; p.b_e = (const uint8_t *)b_s;
     p.out = out; p.ld_out = ld_out; p.out_f32 = out_dtype == MOSS_DT_F32; p.accumulate = accumulate;
     p.e_dwords = 1;
+    if (kind == kBlockSmall64) return b_block == 1 ? launch_mid_kind<kMidBlockRows, 5>(p, st) : launch_mid_kind<kMidBlock, 5>(p, st);
     return b_block == 1 ? launch_mid_kind<kMidBlockRows, 0>(p, st) : launch_mid_kind<kMidBlock, 0>(p, st);
 }

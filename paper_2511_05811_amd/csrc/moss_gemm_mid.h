@@ -53,7 +53,7 @@ struct MidArgs {
 //   kMidBlock       operands with an FP32 scale per 128 of K: per row of a, per 128 rows of b.  A stage is a block of K: its sum is
 //                   taken by unscaled instructions from zero and added to the accumulators times both scales.
 //   kMidBlockRows   the same with a scale per row of b
-//                   (tiles of 32 x 32 only)
+//                   (a fragment per wave only: tiles of 32 x 32, K split over the waves, or of 64 x 64)
 enum MidForm { kMidDense, kMidGroupRows, kMidGroupDw, kMidBlock, kMidBlockRows };
 
 struct MidGroupArgs : MidArgs {
@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kMidThreads) void k_gemm_mx_mid(const MidArgsOf<FOR
         if (FORM == kMidBlockRows) {
 #pragma unroll
             for (int g = 0; g < 4; g++) {
-                const float4 x = *reinterpret_cast<const float4 *>(area_b + at_b + 8 * g + 4 * h);
+                const float4 x = *reinterpret_cast<const float4 *>(area_b + at_b + wn * 32 + 8 * g + 4 * h);
                 sb[4 * g] = x.x; sb[4 * g + 1] = x.y; sb[4 * g + 2] = x.z; sb[4 * g + 3] = x.w;
             }
         }
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kMidThreads) void k_gemm_mx_mid(const MidArgsOf<FOR
         for (int i = 0; i < MI; i++)
 #pragma unroll
             for (int j = 0; j < NJ; j++) {
-                asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]));   // the last matrix instructions retire
+                if (!kBlocked) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[i][j]));   // the last matrix instructions retire
                 store_fragment(acc[i][j], scale, out, p.ld_out, m0 + (wm * MI + i) * 32 + i32, n0 + (wn * NJ + j) * 32, h, M, N, p.out_f32,
                                p.accumulate);
             }
@@ -528,7 +528,7 @@ __global__ __launch_bounds__(kMidThreads) void k_gemm_mx_mid(const MidArgsOf<FOR
     // chunks XOR-swizzled by row), then a thread adds the KS parts of four columns of a row in order, scales and stores.
     // (accumulator register v of lane (i32, h): row i32, column 8 (v / 4) + 4 h + v % 4)
     if (kFrags == 1) {
-        static_assert(kFrags > 1 || (WM * WN == 1 && S::kBM * S::kBN == 4 * kMidThreads), "four outputs per thread");
+        static_assert(kFrags > 1 || KS == 1 || (WM * WN == 1 && S::kBM * S::kBN == 4 * kMidThreads), "four outputs per thread");
         constexpr int kPart = 32 * 32;               // floats per wave
         if (!kBlocked) asm volatile("s_nop 15\n\ts_nop 15" : "+a"(acc[0][0]));   // the last matrix instructions retire
         __syncthreads();                             // slots and exponents have been read
@@ -631,7 +631,8 @@ static int launch_mid_kind(const MidArgsOf<FORM> &p, hipStream_t st)
     else if constexpr (KIND == 1) return launch_mid<FORM, 2, 2, 1, 1, 4, 2>(p, 160 * 1024, st);
     else if constexpr (KIND == 2) return launch_mid<FORM, 2, 2, 1, 2, 2, 3>(p, 160 * 1024, st);
     else if constexpr (KIND == 3) return launch_mid<FORM, 2, 2, 2, 2, 1, 4>(p, 160 * 1024, st);
-    else return launch_mid<FORM, 2, 3, 2, 2, 1, 3>(p, 160 * 1024, st);
+    else if constexpr (KIND == 4) return launch_mid<FORM, 2, 3, 2, 2, 1, 3>(p, 160 * 1024, st);
+    else return launch_mid<FORM, 1, 1, 2, 2, 1, 4>(p, 80 * 1024, st);                           // blocks: a fragment per wave
 }
 
 }  // namespace moss

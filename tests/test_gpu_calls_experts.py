@@ -120,3 +120,28 @@ def test_native_and_python_calls_agree(monkeypatch, data, name):
     native, python = both(monkeypatch, lambda: CALLS[name](data))
     torch.cuda.synchronize()
     same(native, python)
+
+
+WEIGHT_CALLS = {
+    "weight": lambda w: moss.quant_block128_weight(w),
+    "transposed": lambda w: moss.quant_block128_weight(w, True),
+    "BF16": lambda w: moss.quant_block128_weight(w.bfloat16(), want_transpose=True),
+    "outputs given": lambda w: moss.quant_block128_weight(w, True, *moss.quant_block128_weight(w * 2, True)),
+    "the transposed output alone asks for it": lambda w: moss.quant_block128_weight(w, wq_t=torch.zeros(256, 288, dtype=torch.uint8, device="cuda:0")),
+    "an output of another shape": lambda w: moss.quant_block128_weight(w, wq=torch.zeros(288, 128, dtype=torch.uint8, device="cuda:0")),
+    "a view": lambda w: moss.quant_block128_weight(w[:, :128]),
+    "float16": lambda w: moss.quant_block128_weight(w.half()),
+    "odd height": lambda w: moss.quant_block128_weight(w[:40], True),
+    "odd width": lambda w: moss.quant_block128_weight(w[:, :40].contiguous()),
+    "on the host": lambda w: moss.quant_block128_weight(w.cpu()),
+    "three dimensions": lambda w: moss.quant_block128_weight(w.view(3, 96, 256)),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", list(WEIGHT_CALLS))
+def test_native_and_python_calls_agree_on_weights(monkeypatch, name):
+    w = torch.randn(288, 256, generator=torch.Generator("cuda:0").manual_seed(2), device="cuda:0")
+    native, python = both(monkeypatch, lambda: WEIGHT_CALLS[name](w))
+    torch.cuda.synchronize()
+    same(native, python)

@@ -107,3 +107,22 @@ def test_a_scale_that_is_not_finite_stays_in_its_rows(M, N, K, b_block):
     a_s[rows], b_s[blocks] = float("inf"), float("inf")
     got = moss.gemm_fp8_block128(a, a_s, b, b_s)
     assert torch.equal(got[~rows][:, ~columns], want[~rows][:, ~columns])
+
+
+@pytest.mark.parametrize("M,N,K", [(1152, 1000, 32), (1100, 1288, 96), (257, 4100, 512), (2048, 1001, 1056)])
+@pytest.mark.parametrize("b_block", [1, 128])
+def test_block_products_of_odd_sizes(M, N, K, b_block):
+    """64 x 64 outputs at a time, a fragment per wave"""
+    assert tile("moss_internal_gemm_block_tile", M, N, K, b_block, N) == 64064
+    a, a_s, b, b_s = operands(M, N, K, b_block, M + N + K)
+    d = [to_gpu(t) for t in (a, a_s, b, b_s)]
+    A, B = values(a, a_s, 1), values(b, b_s, b_block)
+    got = moss.gemm_fp8_block128(*d)
+    check_product(got, A, B)
+    again(lambda out: moss.gemm_fp8_block128(*d, out=out), got)
+    wide = torch.full((M, N + 3), 7.0, device=dev())
+    out = moss.gemm_fp8_block128(*d, out=wide[:, :N])
+    check_product(out, A, B)
+    base = out.double().cpu().numpy()
+    check_product(moss.gemm_fp8_block128(*d, out=wide[:, :N], accumulate=True), A, B, base)
+    assert bool((wide[:, N:] == 7.0).all())

@@ -28,9 +28,11 @@ def test_block_products_take_larger_tiles_the_larger_they_are(L, M, N, K, block,
     assert ask(L.moss_internal_gemm_block_tile, M, N, K, 1, N) == row
 
 
-@pytest.mark.parametrize("M,N,K,ld", [(8192, 11008, 96, 11008), (8192, 11004, 4096, 11008), (8192, 11008, 4096, 11012), (8192, 1, 4096, 8)])
-def test_block_products_that_the_wide_tiles_cannot_take(L, M, N, K, ld):
-    assert ask(L.moss_internal_gemm_block_tile, M, N, K, 128, ld) == 32032
+@pytest.mark.parametrize("M,N,K,ld,tile", [(8192, 11008, 96, 11008, 64064), (8192, 11004, 4096, 11008, 64064), (8192, 11008, 4096, 11012, 64064),
+                                           (8192, 1, 4096, 8, 32032), (16, 4096, 64, 4096, 32032), (512, 1001, 1024, 1001, 32032),
+                                           (1152, 3968, 32, 3968, 64064), (256, 4100, 512, 4100, 64064), (1, 11001, 96, 11001, 32032)])
+def test_block_products_that_the_wide_tiles_cannot_take(L, M, N, K, ld, tile):
+    assert ask(L.moss_internal_gemm_block_tile, M, N, K, 128, ld) == ask(L.moss_internal_gemm_block_tile, M, N, K, 1, ld) == tile
 
 
 @pytest.mark.parametrize("rows,N,K,groups,tile", [(4, 384, 2432, 64, 32032), (32, 11008, 4096, 8, 32032), (1003, 768, 1184, 32, 64128),
