@@ -126,3 +126,31 @@ def test_block_products_of_odd_sizes(M, N, K, b_block):
     base = out.double().cpu().numpy()
     check_product(moss.gemm_fp8_block128(*d, out=wide[:, :N], accumulate=True), A, B, base)
     assert bool((wide[:, N:] == 7.0).all())
+
+
+# sizes that go to every kind of tiles; offsets that decrease, lie outside and are no multiples of 32
+@pytest.mark.parametrize("R,N,K,G,expected", [(107, 264, 416, 5, 32032), (1004, 768, 1184, 32, 64128), (900, 2560, 1184, 7, 128128), (1680, 5888, 288, 40, 128256),
+                                              (800, 2056, 512, 12, -128256), (5003, 2056, 1152, 7, -256256)])
+def test_wrong_offsets_write_nothing_outside(R, N, K, G, expected):
+    assert tile("moss_internal_gemm_grouped_tile", R, N, K, G, 1, N) == expected
+    p = Rows([0] * G + [R], N, K)
+    wide = torch.full((R + 128, N), SENTINEL, device=dev(), dtype=torch.bfloat16)
+    held = wide[0, 0].item()
+    rng = np.random.default_rng(R)
+    for offsets in (rng.integers(-2 ** 31, 2 ** 31, G + 1), rng.integers(-50, R + 50, G + 1), np.linspace(R, 0, G + 1)):
+        moss.gemm_fp8_mx_grouped(**p.args(out=wide[64:64 + R], offsets=to_gpu(offsets.astype(np.int32))))
+        torch.cuda.synchronize()
+        assert bool((wide[:64] == held).all()) and bool((wide[64 + R:] == held).all())
+
+
+@pytest.mark.parametrize("R,M,N,G,expected", [(1792, 392, 264, 28, 128128), (2048, 520, 1672, 8, 128256), (672, 1120, 1672, 6, 256256)])
+def test_wrong_offsets_of_weight_gradients_write_nothing_outside(R, M, N, G, expected):
+    assert tile("moss_internal_gemm_grouped_dw_tile", R, M, N, G) == expected
+    p = Dw([0] * G + [R], M, N)
+    wide = torch.full((G + 2, M, N), SENTINEL, device=dev())
+    rng = np.random.default_rng(R)
+    for offsets in (rng.integers(-2 ** 31, 2 ** 31, G + 1), rng.integers(-50, R + 50, G + 1), np.linspace(R, 0, G + 1)):
+        moss.gemm_fp8_mx_grouped_dw(**p.args(out=wide[1:1 + G], offsets=to_gpu(offsets.astype(np.int32))))
+        torch.cuda.synchronize()
+        assert bool((wide[0] == SENTINEL).all()) and bool((wide[-1] == SENTINEL).all())
+        assert bool((wide[1:1 + G] != SENTINEL).all())
