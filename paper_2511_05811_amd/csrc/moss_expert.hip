@@ -44,6 +44,14 @@ __device__ __forceinline__ uint32_t ex_top(uint32_t m, uint4 v)
     return ex_pk_max(m, v.w & 0x7FFF7FFFu);
 }
 
+// The rows of an expert with `total` assignments.  They fit 31 bits (moss_expert_rows, which the capacity is held to), the sum on the
+// way there does not.
+__host__ __device__ __forceinline__ int filled_rows(int total, int multiple)
+{
+    const uint32_t m = (uint32_t)multiple;
+    return (int)(((uint32_t)total + m - 1) / m * m);
+}
+
 // The plan.  A workgroup places a contiguous part of the assignments, and counts all of them per expert for itself: those ahead of its
 // part, its own wave by wave, and those behind.  So the workgroups need nothing of each other.  A scan over experts and waves gives
 // each (wave, expert) its first row; then every wave walks its part again.  Of 64 assignments at a time, those of the same expert are
@@ -93,7 +101,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_expert_plan(const int32_t *__r
             total += c;
         }
         total += behind_us[tid];
-        filled = (total + multiple - 1) / multiple * multiple;
+        filled = filled_rows(total, multiple);
     }
     int upto = filled;
 #pragma unroll
@@ -378,6 +386,9 @@ extern "C" int64_t moss_expert_rows(int64_t tokens, int64_t k, int64_t experts, 
     const int64_t n = tokens * k;
     return (n + (experts < n ? experts : n) * (multiple - 1)) / multiple * multiple;
 }
+
+// The rows that the plan gives an expert with so many assignments (asked by the tests)
+extern "C" int64_t moss_internal_expert_filled(int64_t total, int64_t multiple) { return moss::filled_rows((int)total, (int)multiple); }
 
 extern "C" int moss_expert_plan(const int32_t *experts, int64_t tokens, int64_t k, int64_t n_experts, int64_t multiple, int64_t rows,
                                 int32_t *row_of, int32_t *source, int32_t *offsets, void *stream)
