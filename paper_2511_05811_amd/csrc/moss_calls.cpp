@@ -551,6 +551,7 @@ PyObject *quant_block128(PyObject *, PyObject *const *a, Py_ssize_t n)
         void *stream;
         if (!current_place(device, stream)) return nullptr;
         PLAIN_OR_NONE(all_on(device, {x}));
+        for (const Output *o : {&qr, &sr, &qc, &sc}) PLAIN_OR_NONE(!o->o || all_on(device, {&o->t}));
         void *px = ptr(x);
         auto at = [](const Output &o) { return o.o ? o.t.data_ptr() : nullptr; };
         uint8_t *pqr = (uint8_t *)at(qr), *pqc = (uint8_t *)at(qc);
