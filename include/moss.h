@@ -336,6 +336,7 @@ int moss_quant_block128_weight(const void *w, int w_dtype, int64_t rows, int64_t
  * A block's products are summed by the matrix unit, the blocks in FP32 in order of K (K split in up to four parts, each in order,
  * where the problem is small: the choice goes by sizes alone).  A block whose codes are all zeros adds nothing, whatever its finite
  * scales are; otherwise the product of two scales has to be finite, and with b_block 1 a block's sum times a_s as well.
+ * A scale that is NaN or infinite makes the outputs that it scales NaN or infinite, and no others.
  * Requirements: K % 32 == 0, K <= 2^22; ld_out >= N; 16-byte aligned codes and out. */
 int moss_gemm_fp8_block128(int64_t M, int64_t N, int64_t K, const uint8_t *a_q, const float *a_s, const uint8_t *b_q, const float *b_s,
                            int64_t b_block, void *out, int out_dtype, int64_t ld_out, int accumulate, void *stream);

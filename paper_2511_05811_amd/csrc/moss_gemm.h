@@ -188,8 +188,15 @@ __device__ __forceinline__ void mfma_unscaled(v16f &d, const v8i &x, const v8i &
 {
     asm volatile("v_mfma_f32_32x32x64_f8f6f4 %0, %1, %2, %0" : "+v"(d) : "v"(x), "v"(y));
 }
-// The product of a block's two scales, kept finite so that a block of zeros adds nothing whatever they are
-__device__ __forceinline__ float block_scales(float a, float b) { return __builtin_amdgcn_fmed3f(a * b, 3.402823466e38f, -3.402823466e38f); }
+// The product of a block's two scales.  That of finite ones is kept finite, so that a block of zeros adds nothing whatever they are.  One
+// that is NaN or infinite makes it NaN, so that it shows in all that it scales: scales come here with NaN for infinity
+// (shown_scale, once for each that a tile loads), and these two hand NaN on.
+__device__ __forceinline__ float shown_scale(float s) { return __builtin_fmaf(s, 0.0f, s); }
+__device__ __forceinline__ float block_scales(float a, float b)
+{
+    constexpr float kMost = 3.402823466e38f;
+    return __builtin_elementwise_maximum(__builtin_elementwise_minimum(a * b, kMost), -kMost);
+}
 
 __device__ __forceinline__ void pin() { asm volatile("" ::: "memory"); }
 

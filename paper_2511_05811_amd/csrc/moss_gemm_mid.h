@@ -212,7 +212,7 @@ __global__ __launch_bounds__(kMidThreads) void k_gemm_mx_mid(const MidArgsOf<FOR
                     if (c0 + u * per_row < nc) d[u] = *reinterpret_cast<const uint32_t *>(src + (c0 + u * per_row) * 4);
 #pragma unroll
                 for (int u = 0; u < U; u++)
-                    if (c0 + u * per_row < nc) area[(c0 + u * per_row) * pitch + r] = d[u];
+                    if (c0 + u * per_row < nc) area[(c0 + u * per_row) * pitch + r] = kBlocked ? __float_as_uint(shown_scale(__uint_as_float(d[u]))) : d[u];
             }
         } else {
             // rows that are not dword aligned (e itself is): cut out of two neighbouring dwords where both lie inside the

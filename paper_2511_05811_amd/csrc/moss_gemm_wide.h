@@ -317,7 +317,12 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     auto scale_store = [&](int half) {
         if (s_there)
 #pragma unroll
-            for (int u = 0; u < kBlock; u++) ring[(half * kBlock + u) * S::kRows + tid] = !kBlocked && u == moved ? words[u] << moved_by : words[u];
+            for (int u = 0; u < kBlock; u++) {
+                uint32_t w = words[u];
+                if (!kBlocked && u == moved) w <<= moved_by;
+                if (FORM == kWideBlock) w = __float_as_uint(shown_scale(__uint_as_float(w)));
+                ring[(half * kBlock + u) * S::kRows + tid] = w;
+            }
     };
 
     // ---- what is computed
