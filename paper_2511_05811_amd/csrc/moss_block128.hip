@@ -11,7 +11,7 @@
 // Row groups alone need no tile: 16 lanes per group, wherever it lies.
 //
 // 8192 x 4096, rows / columns / both: 18.3 / 21.8 / 30.5 us (5.5 / 4.7 / 4.5 TB/s; a large copy 5.0); 8192 x 11008 both 75.6 (4.8); an FP32
-// weight of 11008 x 4096 with its transposed codes 55.4 (4.9).  With two IEEE divisions per row and per column, shuffles through LDS and
+// weight of 11008 x 4096 with its transposed codes 55.4 (4.9), without 42.6 (5.3), a BF16 weight 36.9 (4.9) and 24.7 (5.5).  With two IEEE divisions per row and per column, shuffles through LDS and
 // a clamp per value, which the memory does not hide in so short a kernel, both took 36.4 and 81.4.
 #include <type_traits>
 

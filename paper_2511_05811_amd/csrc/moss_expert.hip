@@ -7,9 +7,10 @@
 // per thread, half a wave or a wave per token.  Sums and products in FP32, one rounding to BF16 at the end.  The tensors
 // that a quantizer reads leave their maximum behind, as the other BF16 producers do.
 //
-// 8192 tokens of 4096 columns, two of 64 experts each: plan 9.0 us, dispatch 38.5, combine 37.2, its gradient 74.3, that of dispatch
-// 36.6 (4.3 TB/s over all of them, a large copy 5.0; four chunks of a row under way per thread, two or eight are slower).  64 tokens of
-// 256: 3 to 5 us each, a launch and two or three trips to memory behind one another.
+// 8192 tokens of 4096 columns, two of 64 experts each, one behind the other again and again (median, and the fastest of twelve): plan 9.1 us (8.6),
+// dispatch 47.4 (41.0), combine 39.3 (35.4), its gradient 77.4 (75.9), that of dispatch 39.5 (36.4): 213 (197) for what is 940 MB at
+// least, 4.4 TB/s (4.8), a large copy 5.1; the five calls take 214.  (Four chunks of a row under way per thread, two or eight are slower.)
+// 64 tokens of 256: 3 to 5 us each, a launch and two or three trips to memory behind one another.
 #include "moss_internal.h"
 #include "moss_producer.h"
 

@@ -5,10 +5,11 @@
 // times both scales by the vector unit.  Kernels: the wide tiles (moss_gemm_wide.h) and, where few rows leave them idle and for what they
 // cannot take, the small tiles (moss_gemm_mid.h); a stage is one block in both.
 //
-// Bound, large products: power.  8192 x 11008 x 4096 takes 389 us (1.9 PFLOP/s) on quantized data and 511 on random codes, and neither
-// the waits nor the barriers left out shorten it; the copies are 18 % of it, the additions on the vector unit 11 %, the stores 8 %.
-// (The MOSS product of the same size, whose scales the matrix instruction applies: 322 us.)  Few rows: the weight's bytes, 17 x 11008 x
-// 4096 10.4 us, 4.4 TB/s.
+// Bound, large products: matrix unit and vector unit, which take turns in a stage (moss_gemm_wide.h), and power.  8192 x 11008 x 4096 takes 388 to
+// 408 us (1.8 to 1.9 PFLOP/s; 435 to 455 twelve times back to back) on quantized data and 511 on random codes, and neither the waits nor
+// the barriers left out shorten it; without the copies it takes 18 % less, without the additions on the vector unit 11 %, without the stores 8 %.
+// (The MOSS product of the same size, whose scales the matrix instruction applies: 325 us.)  Few rows: the weight's bytes, 17 x 11008 x
+// 4096 10.4 us, 4.4 TB/s.  dW, 4096 x 4096 x 2016: 46 to 49 us into BF16, 52 into FP32, 66 on top of what is there.
 #include "moss_gemm_mid.h"
 #include "moss_gemm_wide.h"
 

@@ -5,10 +5,12 @@
 // tile, or that there is none for it, from the offsets.  Kernels: the small tiles (moss_gemm_mid.h), the wide ones (moss_gemm_wide.h) and
 // the large-tile kernel (moss_gemm_big.hip).
 //
-// Bound: the weights' bytes for few rows (32 rows of 8 experts 11008 x 4096 71 us, 5.1 TB/s); the matrix unit and power for many (16608 rows of
-// 8 experts 11008 x 4096 667 us, 2.2 PFLOP/s); dW lines fetched twice where rows begin inside them (8 experts 4096 x 4096 over 16608
-// rows 365 us, 1.5 PFLOP/s; over 17280, whose groups begin on lines, 315), and latency per tile where sums are short (32 experts of 64 rows 1024 x 1024
-// 30 us; their output's bytes 13).
+// Bound: the weights' bytes for few rows (32 rows of 8 experts 11008 x 4096 69 to 71 us, 5.2 TB/s; 76 back to back); the matrix unit and power for
+// many (16608 rows of 8 experts 11008 x 4096 667 to 721 us, 2.1 to 2.2 PFLOP/s, 762 to 780 back to back; 4096 x 11008 719; dX from one stacked
+// transposed weight, 4096 x 11008 again, 778; K = 4064, which ends inside a stage, 1169 in 128 x 128 tiles); dW lines fetched twice where
+// rows begin inside them (8 experts 4096 x 4096 over 16608 rows 357 to 365 us into BF16, 1.5 PFLOP/s, 421 into FP32, 511 on top of what is
+// there; over 17280, whose groups begin on lines, 315 into BF16), and latency per tile where sums are short (32 experts of 64 rows 1024 x
+// 1024 29 to 31 us into BF16, 42 into FP32, 76 on top of what is there; the outputs' bytes 13, 25, 49).
 #include "moss_gemm_mid.h"
 #include "moss_gemm_wide.h"
 

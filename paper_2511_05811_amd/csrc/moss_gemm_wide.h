@@ -7,8 +7,11 @@
 //  * Stages go through SLOTS slots of LDS, filled by direct global->LDS copies of 128 bytes per row.  One barrier per stage, behind the
 //    last fragment's reads of a: there the stage's slot is free, for the copies of stage + SLOTS, and the next stage has landed.  Its first fragments
 //    are read behind the last matrix instructions of this one, each b fragment behind the instruction that used its registers
-//    last.  While one wave waits its neighbour on the SIMD computes.  Tiles of up to 128 rows have the registers to hold a whole stage,
-//    and with them all its reads stand ahead of the barrier (kHolds).
+//    last.  While one wave waits its neighbour on the SIMD computes.  Tiles of up to 128 rows hold a whole stage in registers, and
+//    all its reads stand ahead of the barrier (kHolds).  (128 x 256 takes all 256
+//    registers for that: 8 of the form for rows of groups are spilled and 7 of that for dW of groups, with some twenty accesses to scratch
+//    memory each.  256 x 256 with a scale per row of b, which does not hold its stage, spills 2.  Scratch counts in vmcnt with the
+//    copies, behind those that a wait is for: it can make a wait longer, never shorter.)
 //  * Blocked forms: an instruction starts from zero and leaves its sum in one of four parts.  A part is added to the accumulators
 //    times its scales when two further instructions have been issued; the matrix unit takes them one after the other, so it has
 //    retired by then.  This order is all that protects the read; the instructions are volatile asm and a part passes through an
@@ -23,9 +26,10 @@
 //    as well: rows of other groups or of none may hold NaN.)
 //
 // A stage takes (us; blocks of 128 of a weight / of rows / dW of groups) 1.56 / 1.90 / 2.3 to 2.7 in 256 x 256 tiles, 0.95 / 1.19 / 1.2 to
-// 1.4 in 128 x 256, 0.67 / 0.79 in 128 x 128, 0.53 / 0.57 in 64 x 128; the matrix instructions of 256 x 256 alone 1.05.  Bound: power and
-// the vector unit's sums in the blocked forms (matrix unit busy 48 % of the time, no LDS conflicts); the copies for dW, whose rows begin
-// anywhere in a line; LDS reads in the smallest tiles.
+// 1.4 in 128 x 256, 0.67 / 0.79 in 128 x 128, 0.53 / 0.57 in 64 x 128; the matrix instructions of 256 x 256 alone 1.05.  Bound: in the
+// blocked forms matrix and vector unit take turns (256 x 256: 1.05 us of matrix instructions, and one or two vector instructions per
+// output, 0.45 or 0.9 us, make the 1.56 and 1.90; matrix unit busy 48 % of the time, no LDS conflicts), on top of which long runs meet the
+// power limit; the copies for dW, whose rows begin anywhere in a line; LDS reads in the smallest tiles.
 //
 // Operand layout of the instruction: lane (r = lane % 16, q = lane / 16) supplies for row r the bytes K[16q, 16q + 16) in its first four
 // registers and K[64 + 16q, 64 + 16q + 16) in the last four; the 32-wide block q of row r is scaled by byte 0 of the lane's
@@ -379,7 +383,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void k_gemm_wide(const WideArgs p)
     };
     auto fold = [&](int n) { add_part(n, FORM == kWideBlockRows ? sa[n / NJ & 3] : __float_as_uint(both[n / NJ & 1]), row_scale); };
 
-    // Tiles with registers to spare: a wave holds all fragments and scales of its stage and reads those of the next between its matrix
+    // Tiles of up to 128 rows: a wave holds all fragments and scales of its stage and reads those of the next between its matrix
     // instructions.  The barrier is at the head of the stage: there every wave holds it, so that its slot is free, and the next has landed.
     // (Where the fragments of a are fetched one ahead instead, a stage of 64 x 128 took 0.65 us, most of it the trip to LDS.)
     constexpr bool kHolds = MI <= 4 && !(FORM == kWideBlockRows && NJ == 4);
